@@ -141,7 +141,8 @@ def _backward(s):
 
 def _tokens_to_int8(x):
     # the integer nearest to x / scale: quotients next to a half are common (x has 8 bits), so they are held in 64 bits
-    scale = x.float().abs().amax(1) / 127.0
+    # (and so is the scale's own division: by a Python number torch would multiply with a reciprocal rounded to fp32)
+    scale = (x.double().abs().amax(1) / 127.0).float()
     return torch.nan_to_num(torch.round(x.double() / scale.double()[:, None])), scale
 
 
@@ -194,7 +195,7 @@ def work(case):
 def _exact_quantised(x):
     """(integers, scales) in 64 bits; the scale itself is a 32-bit number by definition."""
     x = x.double()
-    scale = (x.abs().max(dim=1, keepdim=True).values.float() / 127.0).double()
+    scale = (x.abs().max(dim=1, keepdim=True).values / 127.0).float().double()
     return torch.where(scale > 0, (x / scale).round(), torch.zeros_like(x)), scale
 
 
