@@ -1,0 +1,113 @@
+/*
+ * weave_ffn.h - C ABI of the dense gated feed-forward block (one expert of weave_moe.h without a router, or a model's
+ * dense layers): its forward pass and its gradient in bf16, and its forward pass in 8-bit integers together with the
+ * 8-bit matrix product and the rounding of rows that it is made of.
+ *
+ * The conventions are those of weave_moe.h: plain C, no exceptions, 0 = WEAVE_OK or a negative WEAVE_ERR_* code that
+ * weave_moe_strerror() names; the caller owns every buffer (the library never allocates device memory) and keeps the
+ * weights, their scales and the workspace alive until the handle is destroyed; device pointers belong to the device
+ * that was current at creation, which has to be current in every call; matrices are row-major and dense, 16-byte
+ * aligned; calls are asynchronous on the given stream and may be captured into a CUDA graph.
+ *   - Calls on one handle use its one workspace: one at a time may be in flight, in the order of one stream or ordered
+ *     by the caller.  That holds for replays of graphs that were captured from the same handle, too.
+ *   - The weights may be changed between calls (by work that the stream orders before the next call); the handle keeps
+ *     nothing computed from them.
+ *   - An output must not overlap an input, a weight, another output or the workspace (WEAVE_ERR_INVALID_ARG).
+ *   - T = 0 is allowed: no rows are read or written (a backward call then fills the weight gradients with zeros).
+ */
+#ifndef WEAVE_FFN_H
+#define WEAVE_FFN_H
+
+#include "weave_moe.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef struct weave_ffn *weave_ffn_t;
+
+/* Types of matrix elements in the calls below. */
+enum { WEAVE_BF16 = 0, WEAVE_F32 = 1, WEAVE_INT8 = 2 };
+
+typedef struct weave_ffn_config {
+    int hidden;          /* H: width of x and of the result; a multiple of 8 (WEAVE_INT8: of 16), at most 65536   */
+    int ffn;             /* I: inner width, same rule                                                             */
+    int max_tokens;      /* largest T of a call (sizes the workspace), at most 4194304                            */
+    int weight_type;     /* WEAVE_BF16 or WEAVE_INT8                                                              */
+    int backward;        /* 1 = weave_ffn_backward() may be called (WEAVE_BF16 only)                              */
+    const void *gate_up; /* device [2I][H]: rows [0,I) gate projection (gets SiLU), rows [I,2I) up projection     */
+    const void *down;    /* device [H][I]                                                                         */
+    const float *gate_up_scale; /* WEAVE_INT8: device fp32 [2I], one scale per row; else NULL                     */
+    const float *down_scale;    /* WEAVE_INT8: device fp32 [H]; else NULL                                         */
+    void *workspace;     /* device scratch of at least weave_ffn_workspace_bytes(); 1024-byte aligned             */
+    size_t workspace_bytes;
+} weave_ffn_config;
+
+/* Bytes of device scratch a handle with this config needs (pure host arithmetic on the five integers; 0 = bad shape). */
+size_t weave_ffn_workspace_bytes(const weave_ffn_config *cfg);
+
+/* Validates the config, encodes the weights' TMA descriptors, zeroes the control words (synchronous). */
+int weave_ffn_create(const weave_ffn_config *cfg, weave_ffn_t *out_handle);
+
+/* out[t] = Wd ( silu(Wg x[t]) (.) Wu x[t] ), x and out bf16 [T][H], 0 <= T <= max_tokens.
+ * WEAVE_BF16: products are summed up in fp32, the gated product is rounded to bf16 (a relative 2^-9 of each value at
+ * most), the result as well.
+ * WEAVE_INT8: x is rounded to 8-bit integers with one scale per token (weave_int8_quantize()), so is the gated product
+ * behind its rounding to bf16; sums of integer products are exact. */
+int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda_stream);
+
+/* The gradients of x, gate_up and down for the gradient dy of out: dx bf16 [T][H], dgate_up bf16 [2I][H], ddown bf16
+ * [H][I], all overwritten.  x is what the forward call was given; nothing else is kept between the two: the gate and up
+ * projections are computed again, together with dy's product with down, in the kernel that needs them.  Each result is
+ * a product of fp32 sums, rounded once; its operands h, d(gate) and d(up) are rounded to bf16 once before it. */
+int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, void *dgate_up, void *ddown, int T,
+                       void *cuda_stream);
+
+/* Synchronises the last stream, returns the device status word (WEAVE_OK, or WEAVE_ERR_TIMEOUT if a bounded in-kernel
+ * wait gave up, after which results are undefined) and clears it. */
+int weave_ffn_status(weave_ffn_t h);
+/* Upper bound in milliseconds for any single in-kernel wait (default 4000). */
+int weave_ffn_set_timeout_ms(weave_ffn_t h, int ms);
+int weave_ffn_last_cuda_error(weave_ffn_t h);
+/* Releases host state.  Does not touch device memory. */
+int weave_ffn_destroy(weave_ffn_t h);
+
+/* ---- 8-bit integers with scales ------------------------------------------------------------- */
+
+/* Rows to 8-bit integers: scale[r] = max|x[r]| / 127 in fp32, q[r][c] = the integer nearest to x[r][c] / scale[r]
+ * (decided exactly, ties to even, within +-127).  x: device, x_type WEAVE_BF16 or WEAVE_F32, [rows][cols]; q: int8
+ * [rows][cols]; scale: fp32 [rows]; any cols >= 1.  A row of zeros has scale 0 and zeros; a row with an inf or a NaN
+ * has scale inf or NaN and zeros, so that what is computed from it is NaN.  Serves activations (rows = tokens) and
+ * weights (rows = output channels).  No handle, no workspace. */
+int weave_int8_quantize(const void *x, int x_type, int rows, int cols, void *q, float *scale, void *cuda_stream);
+
+typedef struct weave_int8_linear *weave_int8_linear_t;
+
+typedef struct weave_int8_linear_config {
+    int in_features;     /* K: a multiple of 16, at most 65536 (sums stay below 2^31)                             */
+    int out_features;    /* N: any number up to 4194304                                                           */
+    int max_tokens;      /* largest T of a call, at most 4194304                                                  */
+    const void *weight;  /* device int8 [N][K]                                                                    */
+    const float *scale;  /* device fp32 [N]                                                                       */
+    void *workspace;     /* device scratch of at least weave_int8_linear_workspace_bytes(); 1024-byte aligned     */
+    size_t workspace_bytes;
+} weave_int8_linear_config;
+
+size_t weave_int8_linear_workspace_bytes(const weave_int8_linear_config *cfg);
+int weave_int8_linear_create(const weave_int8_linear_config *cfg, weave_int8_linear_t *out_handle);
+
+/* out[t][n] = (sum_k q[t][k] weight[n][k]) * (x_scale[t] * scale[n]): the sum in int32, exact; the two products in fp32;
+ * out_type WEAVE_BF16 or WEAVE_F32, [T][N].
+ * x_type WEAVE_INT8: x is q and x_scale its scales.  x_type WEAVE_BF16 or WEAVE_F32: x is rounded by
+ * weave_int8_quantize()'s rule first, into the workspace, and x_scale is NULL. */
+int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, const float *x_scale, void *out,
+                              int out_type, int T, void *cuda_stream);
+int weave_int8_linear_status(weave_int8_linear_t h);
+int weave_int8_linear_set_timeout_ms(weave_int8_linear_t h, int ms);
+int weave_int8_linear_last_cuda_error(weave_int8_linear_t h);
+int weave_int8_linear_destroy(weave_int8_linear_t h);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* WEAVE_FFN_H */

@@ -1,4 +1,5 @@
-"""Python binding of the weave_moe C ABI (include/weave_moe.h).
+"""Python binding of the weave_moe C ABI (include/weave_moe.h); the dense feed-forward block and its 8-bit forms
+(include/weave_ffn.h) are in ffn.py and offered here, too.
 
 Argument marshalling only: every step of the layer runs inside the CUDA library.  PyTorch is
 used for device memory and streams.  There is no CPU or eager fallback: if the shared library
@@ -14,7 +15,9 @@ from typing import Optional
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _SRC_DIR = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libweave_moe.so")
-_SOURCES = ["weave_moe.cu", "weave_kernel.cuh", "weave_stream.cuh", "weave_ptx.cuh"]
+_UNITS = ["weave_moe.cu", "weave_ffn.cu"]
+_SOURCES = _UNITS + ["weave_kernel.cuh", "weave_stream.cuh", "weave_ptx.cuh", "weave_gemm.cuh", "weave_quant.cuh"]
+_HEADERS = ["weave_moe.h", "weave_ffn.h"]
 
 WEAVE_OK = 0
 WEAVE_ERR_INVALID_ARG = -1
@@ -34,13 +37,13 @@ class WeaveError(RuntimeError):
 def build(force: bool = False, verbose: bool = False) -> str:
     """nvcc -gencode arch=compute_100a,code=sm_100a -> libweave_moe.so next to this file."""
     srcs = [os.path.join(_SRC_DIR, s) for s in _SOURCES]
-    hdr = os.path.join(os.path.dirname(_HERE), "include", "weave_moe.h")
-    newest = max(os.path.getmtime(p) for p in srcs + [hdr])
+    hdrs = [os.path.join(os.path.dirname(_HERE), "include", h) for h in _HEADERS]
+    newest = max(os.path.getmtime(p) for p in srcs + hdrs)
     if not force and os.path.exists(LIB_PATH) and os.path.getmtime(LIB_PATH) >= newest:
         return LIB_PATH
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-o", LIB_PATH, srcs[0], "-lcudart"]
+           "-shared", "-Xcompiler", "-fPIC", "-o", LIB_PATH] + srcs[:len(_UNITS)] + ["-lcudart"]
     if verbose:
         cmd.insert(1, "-Xptxas")
         cmd.insert(2, "-v")
@@ -436,3 +439,6 @@ class WeaveMoE:
         self._torch.cuda.synchronize()
         raw = self._trace.cpu().numpy().view(np.uint32)
         return [raw[c, :int(raw[c, -1, 0])] for c in range(raw.shape[0])]
+
+
+from .ffn import GatedFFN, Int8FFN, Int8Linear, ffn_workspace_bytes, int8_linear_workspace_bytes, quantize_rows  # noqa: E402

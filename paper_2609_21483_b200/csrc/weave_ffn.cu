@@ -1,0 +1,538 @@
+// Host side of the dense feed-forward block and of the 8-bit product (include/weave_ffn.h): argument checks, tensor
+// maps, the order of the launches.
+#include "../../include/weave_ffn.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <string.h>
+#include <new>
+
+#include "weave_gemm.cuh"
+#include "weave_quant.cuh"
+
+using namespace weave;
+
+namespace {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+constexpr int kMaxWidth = 65536;
+constexpr int kMaxRows = 1 << 22;
+
+size_t up1024(size_t n) { return (n + 1023) & ~(size_t)1023; }
+
+// what both kinds of handle share
+struct Engine {
+    int device, n_sm;
+    FfnCtl *ctl;
+    unsigned long long timeout_ns;
+    cudaStream_t last_stream;
+    int last_cuda_error;
+    EncodeTiledFn encode;
+};
+
+int cuda_fail(Engine &e, cudaError_t err)
+{
+    e.last_cuda_error = (int)err;
+    return WEAVE_ERR_CUDA;
+}
+
+bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+struct Range { const void *p; size_t n; };
+bool overlap(const Range &a, const Range &b)
+{
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return a.n && b.n && x < y + b.n && y < x + a.n;
+}
+// none of the outputs may touch an input or another output
+bool outputs_clear(const Range *out, int n_out, const Range *in, int n_in)
+{
+    for (int i = 0; i < n_out; ++i) {
+        for (int j = 0; j < n_in; ++j)
+            if (overlap(out[i], in[j])) return false;
+        for (int j = i + 1; j < n_out; ++j)
+            if (overlap(out[i], out[j])) return false;
+    }
+    return true;
+}
+
+template <int kEpi, bool kI8, bool kAMn, bool kBMn>
+cudaError_t size_gemm()
+{
+    return cudaFuncSetAttribute(weave_gemm_kernel<kEpi, kI8, kAMn, kBMn>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmemBytes);
+}
+
+int engine_create(Engine &e, void *workspace)
+{
+    cudaError_t err = cudaGetDevice(&e.device);
+    if (err != cudaSuccess) return WEAVE_ERR_CUDA;
+    int major = 0, smem = 0, sms = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, e.device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, e.device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, e.device) != cudaSuccess)
+        return WEAVE_ERR_CUDA;
+    if (major != 10 || smem < kGemmSmemBytes || sms < 2) return WEAVE_ERR_UNSUPPORTED_DEVICE;
+    e.n_sm = sms & ~1;
+    e.ctl = static_cast<FfnCtl *>(workspace);
+    e.timeout_ns = 4000ull * 1000000ull;
+    e.last_stream = nullptr;
+    e.last_cuda_error = 0;
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult res;
+    err = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &res);
+    if (err != cudaSuccess || !fn || res != cudaDriverEntryPointSuccess) return WEAVE_ERR_UNSUPPORTED_DEVICE;
+    e.encode = reinterpret_cast<EncodeTiledFn>(fn);
+    if ((err = size_gemm<kEpiStore, false, false, false>()) != cudaSuccess || (err = size_gemm<kEpiStore, false, false, true>()) != cudaSuccess ||
+        (err = size_gemm<kEpiStore, false, true, true>()) != cudaSuccess || (err = size_gemm<kEpiGated, false, false, false>()) != cudaSuccess ||
+        (err = size_gemm<kEpiGrad, false, false, false>()) != cudaSuccess || (err = size_gemm<kEpiScaled, true, false, false>()) != cudaSuccess ||
+        (err = size_gemm<kEpiScaledGated, true, false, false>()) != cudaSuccess)
+        return cuda_fail(e, err);
+    return WEAVE_OK;
+}
+
+// The control words follow the workspace's last use on the stream: none yet, so a synchronous clear.
+int engine_clear(Engine &e, size_t bytes)
+{
+    cudaError_t err = cudaMemset(e.ctl, 0, bytes);
+    if (err == cudaSuccess) err = cudaDeviceSynchronize();
+    return err == cudaSuccess ? WEAVE_OK : cuda_fail(e, err);
+}
+
+int engine_status(Engine &e, size_t control_bytes)
+{
+    cudaError_t err = cudaStreamSynchronize(e.last_stream);
+    if (err != cudaSuccess) return cuda_fail(e, err);
+    int st = 0;
+    err = cudaMemcpy(&st, &e.ctl->status, sizeof(st), cudaMemcpyDeviceToHost);
+    if (err != cudaSuccess) return cuda_fail(e, err);
+    if (st != 0) {
+        const int rc = engine_clear(e, control_bytes);
+        if (rc) return rc;
+    }
+    return st;
+}
+
+bool on_its_device(const Engine &e)
+{
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == e.device;
+}
+
+// [rows][cols] row-major, box of box_cols x box_rows
+bool map_2d(const Engine &e, CUtensorMap &m, int type, const void *p, long long rows, long long cols, int box_rows, int box_cols)
+{
+    const int size = type == WEAVE_BF16 ? 2 : type == WEAVE_F32 ? 4 : 1;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)cols * size};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+    const cuuint32_t ones[2] = {1, 1};
+    const CUtensorMapDataType dt = type == WEAVE_BF16  ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                   : type == WEAVE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                                       : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+    return e.encode(&m, dt, 2, const_cast<void *>(p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    box_cols * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// operand whose K runs along the rows' elements: 128 rows x 128 bytes
+bool map_k(const Engine &e, CUtensorMap &m, int type, const void *p, long long rows, long long cols)
+{
+    return map_2d(e, m, type, p, rows, cols, 128, type == WEAVE_INT8 ? 128 : 64);
+}
+// operand whose K runs across the rows (bf16): 64 elements x 64 rows
+bool map_mn(const Engine &e, CUtensorMap &m, const void *p, long long rows, long long cols)
+{
+    return map_2d(e, m, WEAVE_BF16, p, rows, cols, 64, 64);
+}
+
+template <int kEpi, bool kI8, bool kAMn, bool kBMn>
+cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int M, int N, long long K0, long long K1, cudaStream_t stream)
+{
+    constexpr int tile_n = kEpi == kEpiStore || kEpi == kEpiScaled ? 256 : 128;
+    constexpr int step = kI8 ? 128 : 64;
+    a.ctl = e.ctl;
+    a.timeout_ns = e.timeout_ns;
+    a.M = M;
+    a.N = N;
+    a.ksteps[0] = (int)((K0 + step - 1) / step);
+    a.ksteps[1] = (int)((K1 + step - 1) / step);
+    a.b_rank_step = kEpi == kEpiStore || kEpi == kEpiScaled ? 128 : 0;
+    a.tiles_m = (M + 255) / 256;
+    a.tiles_n = (N + tile_n - 1) / tile_n;
+    a.group_m = 8;
+    const long long tiles = (long long)a.tiles_m * a.tiles_n;
+    const int pairs = (int)(tiles < e.n_sm / 2 ? tiles : e.n_sm / 2);
+    weave_gemm_kernel<kEpi, kI8, kAMn, kBMn><<<pairs * 2, kGemmThreads, kGemmSmemBytes, stream>>>(a);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_quant(const Engine *e, const void *x, int type, int rows, int cols, int8_t *q, float *scale, cudaStream_t stream)
+{
+    (void)e;
+    const int grid = rows < 148 * 8 ? rows : 148 * 8;
+    const bool vec = (long long)cols * (type == WEAVE_BF16 ? 2 : 4) % 16 == 0 && aligned(x, 16) && aligned(q, 16);
+    if (type == WEAVE_BF16) {
+        const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(x);
+        if (vec) weave_quant_kernel<__nv_bfloat16, true><<<grid, kQuantThreads, 0, stream>>>(p, q, scale, rows, cols);
+        else weave_quant_kernel<__nv_bfloat16, false><<<grid, kQuantThreads, 0, stream>>>(p, q, scale, rows, cols);
+    } else {
+        const float *p = static_cast<const float *>(x);
+        if (vec) weave_quant_kernel<float, true><<<grid, kQuantThreads, 0, stream>>>(p, q, scale, rows, cols);
+        else weave_quant_kernel<float, false><<<grid, kQuantThreads, 0, stream>>>(p, q, scale, rows, cols);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------------------------ the block
+
+namespace {
+struct FfnLayout {
+    size_t h, dgu, xq, x_scale, hq, h_scale, control, total;
+};
+bool ffn_shape_ok(const weave_ffn_config *c)
+{
+    if (!c || (c->weight_type != WEAVE_BF16 && c->weight_type != WEAVE_INT8)) return false;
+    const int unit = c->weight_type == WEAVE_INT8 ? 16 : 8;
+    return c->hidden > 0 && c->ffn > 0 && c->hidden % unit == 0 && c->ffn % unit == 0 && c->hidden <= kMaxWidth && c->ffn <= kMaxWidth &&
+           c->max_tokens > 0 && c->max_tokens <= kMaxRows && (c->backward == 0 || (c->backward == 1 && c->weight_type == WEAVE_BF16));
+}
+FfnLayout ffn_layout(const weave_ffn_config *c)
+{
+    FfnLayout L;
+    memset(&L, 0, sizeof(L));
+    const size_t T = (size_t)c->max_tokens, H = (size_t)c->hidden, I = (size_t)c->ffn;
+    size_t at = up1024(sizeof(FfnCtl));
+    L.control = at;
+    L.h = at;
+    at += up1024(T * I * 2);
+    if (c->backward) {
+        L.dgu = at;
+        at += up1024(T * 2 * I * 2);
+    }
+    if (c->weight_type == WEAVE_INT8) {
+        L.xq = at;
+        at += up1024(T * H);
+        L.x_scale = at;
+        at += up1024(T * 4);
+        L.hq = at;
+        at += up1024(T * I);
+        L.h_scale = at;
+        at += up1024(T * 4);
+    }
+    L.total = at;
+    return L;
+}
+}  // namespace
+
+struct weave_ffn {
+    Engine e;
+    weave_ffn_config cfg;
+    FfnLayout L;
+    uint8_t *ws;
+    CUtensorMap gate_k, up_k, down_k;          // K along the rows: forward products
+    CUtensorMap gate_up_mn, down_mn;           // K across the rows: backward products
+};
+
+extern "C" {
+
+size_t weave_ffn_workspace_bytes(const weave_ffn_config *cfg)
+{
+    return ffn_shape_ok(cfg) ? ffn_layout(cfg).total : 0;
+}
+
+int weave_ffn_create(const weave_ffn_config *cfg, weave_ffn_t *out)
+{
+    if (!out) return WEAVE_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!ffn_shape_ok(cfg) || !cfg->gate_up || !cfg->down || !cfg->workspace) return WEAVE_ERR_INVALID_ARG;
+    if (!aligned(cfg->gate_up, 16) || !aligned(cfg->down, 16) || !aligned(cfg->workspace, 1024)) return WEAVE_ERR_INVALID_ARG;
+    const bool i8 = cfg->weight_type == WEAVE_INT8;
+    if (i8 != (cfg->gate_up_scale != nullptr) || i8 != (cfg->down_scale != nullptr)) return WEAVE_ERR_INVALID_ARG;
+    if (!aligned(cfg->gate_up_scale, 4) || !aligned(cfg->down_scale, 4)) return WEAVE_ERR_INVALID_ARG;
+    const FfnLayout L = ffn_layout(cfg);
+    if (cfg->workspace_bytes < L.total) return WEAVE_ERR_WORKSPACE;
+    weave_ffn *h = new (std::nothrow) weave_ffn();
+    if (!h) return WEAVE_ERR_INVALID_ARG;
+    h->cfg = *cfg;
+    h->L = L;
+    h->ws = static_cast<uint8_t *>(cfg->workspace);
+    int rc = engine_create(h->e, cfg->workspace);
+    if (rc == WEAVE_OK) {
+        const int H = cfg->hidden, I = cfg->ffn, type = cfg->weight_type;
+        const uint8_t *up = static_cast<const uint8_t *>(cfg->gate_up) + (size_t)I * H * (i8 ? 1 : 2);
+        bool ok = map_k(h->e, h->gate_k, type, cfg->gate_up, I, H) && map_k(h->e, h->up_k, type, up, I, H) &&
+                  map_k(h->e, h->down_k, type, cfg->down, H, I);
+        if (cfg->backward) ok = ok && map_mn(h->e, h->gate_up_mn, cfg->gate_up, 2ll * I, H) && map_mn(h->e, h->down_mn, cfg->down, H, I);
+        rc = ok ? engine_clear(h->e, L.control) : WEAVE_ERR_CUDA;
+    }
+    if (rc != WEAVE_OK) {
+        delete h;
+        return rc;
+    }
+    *out = h;
+    return WEAVE_OK;
+}
+
+int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda_stream)
+{
+    if (!h || T < 0 || T > h->cfg.max_tokens) return WEAVE_ERR_INVALID_ARG;
+    if (T == 0) return WEAVE_OK;
+    const int H = h->cfg.hidden, I = h->cfg.ffn;
+    if (!x || !out || !aligned(x, 16) || !aligned(out, 16)) return WEAVE_ERR_INVALID_ARG;
+    const size_t wsize = h->cfg.weight_type == WEAVE_INT8 ? 1 : 2, rows = (size_t)T * H * 2;
+    const Range outs[1] = {{out, rows}};
+    const Range ins[4] = {{x, rows}, {h->cfg.gate_up, (size_t)2 * I * H * wsize}, {h->cfg.down, (size_t)I * H * wsize}, {h->ws, h->L.total}};
+    if (!outputs_clear(outs, 1, ins, 4) || !on_its_device(h->e)) return WEAVE_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    h->e.last_stream = stream;
+    uint8_t *hbuf = h->ws + h->L.h;
+    cudaError_t err;
+    GemmArgs g, d;
+    if (h->cfg.weight_type == WEAVE_BF16) {
+        if (!map_k(h->e, g.a[0], WEAVE_BF16, x, T, H) || !map_2d(h->e, g.d[0], WEAVE_BF16, hbuf, T, I, 32, 64) ||
+            !map_k(h->e, d.a[0], WEAVE_BF16, hbuf, T, I) || !map_2d(h->e, d.d[0], WEAVE_BF16, out, T, H, 32, 64))
+            return WEAVE_ERR_CUDA;
+        g.b[0][0] = h->gate_k;
+        g.b[0][1] = h->up_k;
+        err = launch_gemm<kEpiGated, false, false, false>(h->e, g, T, I, H, 0, stream);
+        if (err != cudaSuccess) return cuda_fail(h->e, err);
+        d.b[0][0] = d.b[0][1] = h->down_k;
+        err = launch_gemm<kEpiStore, false, false, false>(h->e, d, T, H, I, 0, stream);
+        return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
+    }
+    int8_t *xq = reinterpret_cast<int8_t *>(h->ws + h->L.xq), *hq = reinterpret_cast<int8_t *>(h->ws + h->L.hq);
+    float *xs = reinterpret_cast<float *>(h->ws + h->L.x_scale), *hs = reinterpret_cast<float *>(h->ws + h->L.h_scale);
+    if (!map_k(h->e, g.a[0], WEAVE_INT8, xq, T, H) || !map_2d(h->e, g.d[0], WEAVE_BF16, hbuf, T, I, 32, 64) ||
+        !map_k(h->e, d.a[0], WEAVE_INT8, hq, T, I) || !map_2d(h->e, d.d[0], WEAVE_BF16, out, T, H, 32, 64))
+        return WEAVE_ERR_CUDA;
+    err = launch_quant(&h->e, x, WEAVE_BF16, T, H, xq, xs, stream);
+    if (err != cudaSuccess) return cuda_fail(h->e, err);
+    g.b[0][0] = h->gate_k;
+    g.b[0][1] = h->up_k;
+    g.row_scale = xs;
+    g.col_scale = h->cfg.gate_up_scale;
+    err = launch_gemm<kEpiScaledGated, true, false, false>(h->e, g, T, I, H, 0, stream);
+    if (err != cudaSuccess) return cuda_fail(h->e, err);
+    err = launch_quant(&h->e, hbuf, WEAVE_BF16, T, I, hq, hs, stream);
+    if (err != cudaSuccess) return cuda_fail(h->e, err);
+    d.b[0][0] = d.b[0][1] = h->down_k;
+    d.row_scale = hs;
+    d.col_scale = h->cfg.down_scale;
+    d.out_f32 = d.direct = 0;
+    err = launch_gemm<kEpiScaled, true, false, false>(h->e, d, T, H, I, 0, stream);
+    return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
+}
+
+int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, void *dgate_up, void *ddown, int T, void *cuda_stream)
+{
+    if (!h || !h->cfg.backward || T < 0 || T > h->cfg.max_tokens) return WEAVE_ERR_INVALID_ARG;
+    if (!dgate_up || !ddown || !aligned(dgate_up, 16) || !aligned(ddown, 16)) return WEAVE_ERR_INVALID_ARG;
+    if (T > 0 && (!x || !dy || !dx || !aligned(x, 16) || !aligned(dy, 16) || !aligned(dx, 16))) return WEAVE_ERR_INVALID_ARG;
+    const int H = h->cfg.hidden, I = h->cfg.ffn;
+    const size_t rows = (size_t)T * H * 2, w_gu = (size_t)2 * I * H * 2, w_d = (size_t)I * H * 2;
+    const Range outs[3] = {{dx, rows}, {dgate_up, w_gu}, {ddown, w_d}};
+    const Range ins[5] = {{x, rows}, {dy, rows}, {h->cfg.gate_up, w_gu}, {h->cfg.down, w_d}, {h->ws, h->L.total}};
+    if (!outputs_clear(outs, 3, ins, 5) || !on_its_device(h->e)) return WEAVE_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    h->e.last_stream = stream;
+    cudaError_t err;
+    if (T == 0) {
+        err = cudaMemsetAsync(dgate_up, 0, w_gu, stream);
+        if (err == cudaSuccess) err = cudaMemsetAsync(ddown, 0, w_d, stream);
+        return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
+    }
+    uint8_t *hbuf = h->ws + h->L.h, *dgu = h->ws + h->L.dgu;
+    // h and [dg du] from x and dy
+    GemmArgs g;
+    bool ok = map_k(h->e, g.a[0], WEAVE_BF16, dy, T, H) && map_k(h->e, g.a[1], WEAVE_BF16, x, T, H) &&
+              map_2d(h->e, g.d[0], WEAVE_BF16, hbuf, T, I, 32, 32);
+    // d(gate) and d(up) lie side by side in rows of 2I; their maps end where their half ends
+    const cuuint64_t dims[2] = {(cuuint64_t)I, (cuuint64_t)T}, strides[1] = {(cuuint64_t)I * 4};
+    const cuuint32_t box[2] = {32, 32}, ones[2] = {1, 1};
+    for (int half = 0; half < 2 && ok; ++half)
+        ok = h->e.encode(&g.d[1 + half], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dgu + (size_t)half * I * 2, dims, strides, box, ones,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    if (!ok) return WEAVE_ERR_CUDA;
+    g.b[0][0] = g.b[0][1] = h->down_mn;
+    g.b[1][0] = h->gate_k;
+    g.b[1][1] = h->up_k;
+    err = launch_gemm<kEpiGrad, false, false, false>(h->e, g, T, I, H, H, stream);
+    if (err != cudaSuccess) return cuda_fail(h->e, err);
+    // dx = [dg du] W_gu
+    if (!map_k(h->e, g.a[0], WEAVE_BF16, dgu, T, 2ll * I) || !map_2d(h->e, g.d[0], WEAVE_BF16, dx, T, H, 32, 64)) return WEAVE_ERR_CUDA;
+    g.b[0][0] = g.b[0][1] = h->gate_up_mn;
+    err = launch_gemm<kEpiStore, false, false, true>(h->e, g, T, H, 2ll * I, 0, stream);
+    if (err != cudaSuccess) return cuda_fail(h->e, err);
+    // dW_gu = [dg du]^T x
+    if (!map_mn(h->e, g.a[0], dgu, T, 2ll * I) || !map_mn(h->e, g.b[0][0], x, T, H) ||
+        !map_2d(h->e, g.d[0], WEAVE_BF16, dgate_up, 2ll * I, H, 32, 64))
+        return WEAVE_ERR_CUDA;
+    g.b[0][1] = g.b[0][0];
+    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, 2 * I, H, T, 0, stream);
+    if (err != cudaSuccess) return cuda_fail(h->e, err);
+    // dW_d = dy^T h
+    if (!map_mn(h->e, g.a[0], dy, T, H) || !map_mn(h->e, g.b[0][0], hbuf, T, I) || !map_2d(h->e, g.d[0], WEAVE_BF16, ddown, H, I, 32, 64))
+        return WEAVE_ERR_CUDA;
+    g.b[0][1] = g.b[0][0];
+    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, H, I, T, 0, stream);
+    return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
+}
+
+int weave_ffn_status(weave_ffn_t h) { return h ? engine_status(h->e, h->L.control) : WEAVE_ERR_INVALID_ARG; }
+
+int weave_ffn_set_timeout_ms(weave_ffn_t h, int ms)
+{
+    if (!h || ms <= 0) return WEAVE_ERR_INVALID_ARG;
+    h->e.timeout_ns = (unsigned long long)ms * 1000000ull;
+    return WEAVE_OK;
+}
+
+int weave_ffn_last_cuda_error(weave_ffn_t h) { return h ? h->e.last_cuda_error : 0; }
+
+int weave_ffn_destroy(weave_ffn_t h)
+{
+    delete h;
+    return WEAVE_OK;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------------------------ 8-bit integers
+
+namespace {
+struct Int8Layout { size_t xq, x_scale, control, total; };
+bool int8_shape_ok(const weave_int8_linear_config *c)
+{
+    return c && c->in_features > 0 && c->in_features % 16 == 0 && c->in_features <= kMaxWidth && c->out_features > 0 &&
+           c->out_features <= kMaxRows && c->max_tokens > 0 && c->max_tokens <= kMaxRows;
+}
+Int8Layout int8_layout(const weave_int8_linear_config *c)
+{
+    Int8Layout L;
+    size_t at = up1024(sizeof(FfnCtl));
+    L.control = at;
+    L.xq = at;
+    at += up1024((size_t)c->max_tokens * c->in_features);
+    L.x_scale = at;
+    at += up1024((size_t)c->max_tokens * 4);
+    L.total = at;
+    return L;
+}
+}  // namespace
+
+struct weave_int8_linear {
+    Engine e;
+    weave_int8_linear_config cfg;
+    Int8Layout L;
+    uint8_t *ws;
+    CUtensorMap weight_k;
+};
+
+extern "C" {
+
+int weave_int8_quantize(const void *x, int x_type, int rows, int cols, void *q, float *scale, void *cuda_stream)
+{
+    if ((x_type != WEAVE_BF16 && x_type != WEAVE_F32) || rows < 0 || cols < 1) return WEAVE_ERR_INVALID_ARG;
+    if (rows == 0) return WEAVE_OK;
+    const size_t size = x_type == WEAVE_BF16 ? 2 : 4, n = (size_t)rows * cols;
+    if (!x || !q || !scale || !aligned(x, size) || !aligned(scale, 4)) return WEAVE_ERR_INVALID_ARG;
+    const Range outs[2] = {{q, n}, {scale, (size_t)rows * 4}}, ins[1] = {{x, n * size}};
+    if (!outputs_clear(outs, 2, ins, 1)) return WEAVE_ERR_INVALID_ARG;
+    return launch_quant(nullptr, x, x_type, rows, cols, static_cast<int8_t *>(q), scale, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+               ? WEAVE_OK
+               : WEAVE_ERR_CUDA;
+}
+
+size_t weave_int8_linear_workspace_bytes(const weave_int8_linear_config *cfg)
+{
+    return int8_shape_ok(cfg) ? int8_layout(cfg).total : 0;
+}
+
+int weave_int8_linear_create(const weave_int8_linear_config *cfg, weave_int8_linear_t *out)
+{
+    if (!out) return WEAVE_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!int8_shape_ok(cfg) || !cfg->weight || !cfg->scale || !cfg->workspace) return WEAVE_ERR_INVALID_ARG;
+    if (!aligned(cfg->weight, 16) || !aligned(cfg->scale, 4) || !aligned(cfg->workspace, 1024)) return WEAVE_ERR_INVALID_ARG;
+    const Int8Layout L = int8_layout(cfg);
+    if (cfg->workspace_bytes < L.total) return WEAVE_ERR_WORKSPACE;
+    weave_int8_linear *h = new (std::nothrow) weave_int8_linear();
+    if (!h) return WEAVE_ERR_INVALID_ARG;
+    h->cfg = *cfg;
+    h->L = L;
+    h->ws = static_cast<uint8_t *>(cfg->workspace);
+    int rc = engine_create(h->e, cfg->workspace);
+    if (rc == WEAVE_OK)
+        rc = map_k(h->e, h->weight_k, WEAVE_INT8, cfg->weight, cfg->out_features, cfg->in_features) ? engine_clear(h->e, L.control)
+                                                                                                    : WEAVE_ERR_CUDA;
+    if (rc != WEAVE_OK) {
+        delete h;
+        return rc;
+    }
+    *out = h;
+    return WEAVE_OK;
+}
+
+int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, const float *x_scale, void *out, int out_type, int T,
+                              void *cuda_stream)
+{
+    if (!h || T < 0 || T > h->cfg.max_tokens || (out_type != WEAVE_BF16 && out_type != WEAVE_F32) ||
+        (x_type != WEAVE_BF16 && x_type != WEAVE_F32 && x_type != WEAVE_INT8) || (x_type == WEAVE_INT8) != (x_scale != nullptr))
+        return WEAVE_ERR_INVALID_ARG;
+    if (T == 0) return WEAVE_OK;
+    if (!x || !out || !aligned(x, 16) || !aligned(out, 16) || !aligned(x_scale, 4)) return WEAVE_ERR_INVALID_ARG;
+    const int K = h->cfg.in_features, N = h->cfg.out_features;
+    const size_t out_size = out_type == WEAVE_F32 ? 4 : 2, x_size = x_type == WEAVE_INT8 ? 1 : x_type == WEAVE_BF16 ? 2 : 4;
+    const Range outs[1] = {{out, (size_t)T * N * out_size}};
+    const Range ins[5] = {{x, (size_t)T * K * x_size}, {x_scale, x_scale ? (size_t)T * 4 : 0}, {h->cfg.weight, (size_t)N * K},
+                          {h->cfg.scale, (size_t)N * 4}, {h->ws, h->L.total}};
+    if (!outputs_clear(outs, 1, ins, 5) || !on_its_device(h->e)) return WEAVE_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    h->e.last_stream = stream;
+    const void *q = x;
+    cudaError_t err;
+    if (x_type != WEAVE_INT8) {
+        int8_t *xq = reinterpret_cast<int8_t *>(h->ws + h->L.xq);
+        float *xs = reinterpret_cast<float *>(h->ws + h->L.x_scale);
+        err = launch_quant(&h->e, x, x_type, T, K, xq, xs, stream);
+        if (err != cudaSuccess) return cuda_fail(h->e, err);
+        q = xq;
+        x_scale = xs;
+    }
+    GemmArgs g;
+    g.direct = (size_t)N * out_size % 16 != 0;
+    g.out_f32 = out_type == WEAVE_F32;
+    g.out = out;
+    g.ld_out = N;
+    g.row_scale = x_scale;
+    g.col_scale = h->cfg.scale;
+    if (!map_k(h->e, g.a[0], WEAVE_INT8, q, T, K)) return WEAVE_ERR_CUDA;
+    if (!g.direct && !map_2d(h->e, g.d[0], out_type, out, T, N, 32, out_type == WEAVE_F32 ? 32 : 64)) return WEAVE_ERR_CUDA;
+    g.b[0][0] = g.b[0][1] = h->weight_k;
+    err = launch_gemm<kEpiScaled, true, false, false>(h->e, g, T, N, K, 0, stream);
+    return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
+}
+
+int weave_int8_linear_status(weave_int8_linear_t h) { return h ? engine_status(h->e, h->L.control) : WEAVE_ERR_INVALID_ARG; }
+
+int weave_int8_linear_set_timeout_ms(weave_int8_linear_t h, int ms)
+{
+    if (!h || ms <= 0) return WEAVE_ERR_INVALID_ARG;
+    h->e.timeout_ns = (unsigned long long)ms * 1000000ull;
+    return WEAVE_OK;
+}
+
+int weave_int8_linear_last_cuda_error(weave_int8_linear_t h) { return h ? h->e.last_cuda_error : 0; }
+
+int weave_int8_linear_destroy(weave_int8_linear_t h)
+{
+    delete h;
+    return WEAVE_OK;
+}
+
+}  // extern "C"
