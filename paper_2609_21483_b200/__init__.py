@@ -16,7 +16,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _SRC_DIR = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libweave_moe.so")
 _UNITS = ["weave_moe.cu", "weave_ffn.cu"]
-_SOURCES = _UNITS + ["weave_kernel.cuh", "weave_stream.cuh", "weave_ptx.cuh", "weave_gemm.cuh", "weave_quant.cuh"]
+_SOURCES = _UNITS + ["weave_kernel.cuh", "weave_stream.cuh", "weave_ptx.cuh", "weave_gemm.cuh",
+                     "weave_ffn_stream.cuh", "weave_quant.cuh"]
 _HEADERS = ["weave_moe.h", "weave_ffn.h"]
 
 WEAVE_OK = 0

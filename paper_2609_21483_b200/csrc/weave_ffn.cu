@@ -7,6 +7,7 @@
 #include <string.h>
 #include <new>
 
+#include "weave_ffn_stream.cuh"
 #include "weave_gemm.cuh"
 #include "weave_quant.cuh"
 
@@ -31,6 +32,8 @@ struct Engine {
     cudaStream_t last_stream;
     int last_cuda_error;
     EncodeTiledFn encode;
+    unsigned *arrived;         // streaming kernel: arrivals per tile, and partial sums
+    uint32_t *partials;
 };
 
 int cuda_fail(Engine &e, cudaError_t err)
@@ -59,10 +62,30 @@ bool outputs_clear(const Range *out, int n_out, const Range *in, int n_in)
     return true;
 }
 
+// Scratch of the streaming kernel for the largest of a handle's products (N columns of the result, 128 of them in a
+// tile if they are gated).  Behind the control words, which creation clears.
+constexpr int kStreamCtas = 148;
+struct StreamScratch { size_t arrived, partials; };
+StreamScratch stream_scratch(int max_tokens, long long tiles, long long units)
+{
+    const long long T = max_tokens < kFfnStreamMaxT ? max_tokens : kFfnStreamMaxT;
+    const long long ctas = units < kStreamCtas ? units : kStreamCtas;
+    StreamScratch s;
+    s.arrived = (size_t)tiles * 4;
+    s.partials = (size_t)(2 * ctas * 256 * T * 4);
+    return s;
+}
+
 template <int kEpi, bool kI8, bool kAMn, bool kBMn>
 cudaError_t size_gemm()
 {
     return cudaFuncSetAttribute(weave_gemm_kernel<kEpi, kI8, kAMn, kBMn>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmemBytes);
+}
+
+template <bool kI8, bool kGated>
+cudaError_t size_stream()
+{
+    return cudaFuncSetAttribute(weave_ffn_stream_kernel<kI8, kGated>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFfnStreamSmem);
 }
 
 int engine_create(Engine &e, void *workspace)
@@ -88,7 +111,9 @@ int engine_create(Engine &e, void *workspace)
     if ((err = size_gemm<kEpiStore, false, false, false>()) != cudaSuccess || (err = size_gemm<kEpiStore, false, false, true>()) != cudaSuccess ||
         (err = size_gemm<kEpiStore, false, true, true>()) != cudaSuccess || (err = size_gemm<kEpiGated, false, false, false>()) != cudaSuccess ||
         (err = size_gemm<kEpiGrad, false, false, false>()) != cudaSuccess || (err = size_gemm<kEpiScaled, true, false, false>()) != cudaSuccess ||
-        (err = size_gemm<kEpiScaledGated, true, false, false>()) != cudaSuccess)
+        (err = size_gemm<kEpiScaledGated, true, false, false>()) != cudaSuccess || (err = size_stream<false, false>()) != cudaSuccess ||
+        (err = size_stream<false, true>()) != cudaSuccess || (err = size_stream<true, false>()) != cudaSuccess ||
+        (err = size_stream<true, true>()) != cudaSuccess)
         return cuda_fail(e, err);
     return WEAVE_OK;
 }
@@ -141,14 +166,97 @@ bool map_k(const Engine &e, CUtensorMap &m, int type, const void *p, long long r
 {
     return map_2d(e, m, type, p, rows, cols, 128, type == WEAVE_INT8 ? 128 : 64);
 }
+// tokens' box of the streaming kernel (the N of its MMA)
+int stream_box(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
+bool map_stream_x(const Engine &e, CUtensorMap &m, int type, const void *p, int T, long long cols)
+{
+    return map_2d(e, m, type, p, T, cols, stream_box(T), type == WEAVE_INT8 ? 128 : 64);
+}
+// weights of the streaming kernel: 256 rows, or 128 rows of each of two halves of `rows` rows
+bool map_stream_w(const Engine &e, CUtensorMap &m, int type, const void *p, long long rows, long long cols, bool gated)
+{
+    if (!gated) return map_2d(e, m, type, p, rows, cols, 256, type == WEAVE_INT8 ? 128 : 64);
+    const int size = type == WEAVE_INT8 ? 1 : 2;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, 2};
+    const cuuint64_t strides[2] = {(cuuint64_t)cols * size, (cuuint64_t)rows * cols * size};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / size), 128, 2}, ones[3] = {1, 1, 1};
+    return e.encode(&m, size == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides,
+                    box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 // operand whose K runs across the rows (bf16): 64 elements x 64 rows
 bool map_mn(const Engine &e, CUtensorMap &m, const void *p, long long rows, long long cols)
 {
     return map_2d(e, m, WEAVE_BF16, p, rows, cols, 64, 64);
 }
 
+#ifndef WEAVE_STREAM_T
+#define WEAVE_STREAM_T kFfnStreamMaxT
+#endif
+bool use_stream(int T) { return T <= WEAVE_STREAM_T; }
+
+// behind: launched while the launch before it in the stream, one of the same call, still runs (see pdl_wait())
+template <class... Params, class... Args>
+cudaError_t launch(void (*kernel)(Params...), int grid, int block, size_t smem, bool behind, cudaStream_t stream, const Args &...args)
+{
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3(grid);
+    lc.blockDim = dim3(block);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = stream;
+    lc.attrs = &at;
+    lc.numAttrs = behind ? 1 : 0;
+    return cudaLaunchKernelEx(&lc, kernel, args...);
+}
+
+// Units of work per CTA of the streaming kernel.  A CTA takes about 430 cycles per unit of 32 KB on its own and the
+// chip 10 cycles per unit in all; a shared tile costs its last CTA a round trip and the reading of 1 KB per segment and
+// token.
+int stream_units_per_cta(int T, int ksteps, int tiles, int ctas)
+{
+    const long long units = (long long)ksteps * tiles;
+    const int least = (int)((units + ctas - 1) / ctas);
+    int best = least;
+    double best_cost = 1e30;
+    for (int u = least; u <= (least > ksteps ? least : ksteps); ++u) {
+        const int shared = u % ksteps == 0 ? 1 : ksteps % u == 0 ? ksteps / u : (ksteps + u - 1) / u + 1;
+        const double load = u * 430.0 > units * 10.0 ? u * 430.0 : units * 10.0;
+        const double cost = load + (shared > 1 ? 2500.0 + shared * (T * 16.0 + 50.0) : 0.0);
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = u;
+        }
+    }
+    return best;
+}
+
+template <bool kI8, bool kGated>
+cudaError_t launch_stream(const Engine &e, FfnStreamArgs &a, int T, int N, long long K, bool behind, cudaStream_t stream)
+{
+    a.ctl = e.ctl;
+    a.timeout_ns = e.timeout_ns;
+    a.arrived = e.arrived;
+    a.partials = e.partials;
+    a.T = T;
+    a.N = N;
+    a.ld_out = N;
+    a.ksteps = (int)((K + (kI8 ? 127 : 63)) / (kI8 ? 128 : 64));
+    a.tiles = (N + (kGated ? 127 : 255)) / (kGated ? 128 : 256);
+    a.units = a.ksteps * a.tiles;
+    const int ctas = e.n_sm < kStreamCtas ? e.n_sm : kStreamCtas;
+    a.units_per_cta = stream_units_per_cta(T, a.ksteps, a.tiles, ctas);
+    a.box_t = stream_box(T);
+    a.stages = ffn_stream_stages(a.box_t);
+    const size_t smem = 1024 + (size_t)a.stages * (kFfnStreamWeights + a.box_t * 128) + sizeof(FfnStreamBars);
+    return launch(weave_ffn_stream_kernel<kI8, kGated>, (a.units + a.units_per_cta - 1) / a.units_per_cta, kFfnStreamThreads, smem, behind,
+                  stream, a);
+}
+
 template <int kEpi, bool kI8, bool kAMn, bool kBMn>
-cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int M, int N, long long K0, long long K1, cudaStream_t stream)
+cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int M, int N, long long K0, long long K1, bool behind, cudaStream_t stream)
 {
     constexpr int tile_n = kEpi == kEpiStore || kEpi == kEpiScaled ? 256 : 128;
     constexpr int step = kI8 ? 128 : 64;
@@ -164,25 +272,22 @@ cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int M, int N, long long K0
     a.group_m = 8;
     const long long tiles = (long long)a.tiles_m * a.tiles_n;
     const int pairs = (int)(tiles < e.n_sm / 2 ? tiles : e.n_sm / 2);
-    weave_gemm_kernel<kEpi, kI8, kAMn, kBMn><<<pairs * 2, kGemmThreads, kGemmSmemBytes, stream>>>(a);
-    return cudaGetLastError();
+    return launch(weave_gemm_kernel<kEpi, kI8, kAMn, kBMn>, pairs * 2, kGemmThreads, kGemmSmemBytes, behind, stream, a);
 }
 
-cudaError_t launch_quant(const Engine *e, const void *x, int type, int rows, int cols, int8_t *q, float *scale, cudaStream_t stream)
+cudaError_t launch_quant(const void *x, int type, int rows, int cols, int8_t *q, float *scale, bool behind, cudaStream_t stream)
 {
-    (void)e;
     const int grid = rows < 148 * 8 ? rows : 148 * 8;
     const bool vec = (long long)cols * (type == WEAVE_BF16 ? 2 : 4) % 16 == 0 && aligned(x, 16) && aligned(q, 16);
+    const long long r = rows, c = cols;
     if (type == WEAVE_BF16) {
         const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(x);
-        if (vec) weave_quant_kernel<__nv_bfloat16, true><<<grid, kQuantThreads, 0, stream>>>(p, q, scale, rows, cols);
-        else weave_quant_kernel<__nv_bfloat16, false><<<grid, kQuantThreads, 0, stream>>>(p, q, scale, rows, cols);
-    } else {
-        const float *p = static_cast<const float *>(x);
-        if (vec) weave_quant_kernel<float, true><<<grid, kQuantThreads, 0, stream>>>(p, q, scale, rows, cols);
-        else weave_quant_kernel<float, false><<<grid, kQuantThreads, 0, stream>>>(p, q, scale, rows, cols);
+        return launch(vec ? weave_quant_kernel<__nv_bfloat16, true> : weave_quant_kernel<__nv_bfloat16, false>, grid, kQuantThreads, 0, behind,
+                      stream, p, q, scale, r, c);
     }
-    return cudaGetLastError();
+    const float *p = static_cast<const float *>(x);
+    return launch(vec ? weave_quant_kernel<float, true> : weave_quant_kernel<float, false>, grid, kQuantThreads, 0, behind, stream, p, q, scale,
+                  r, c);
 }
 
 }  // namespace
@@ -191,7 +296,7 @@ cudaError_t launch_quant(const Engine *e, const void *x, int type, int rows, int
 
 namespace {
 struct FfnLayout {
-    size_t h, dgu, xq, x_scale, hq, h_scale, control, total;
+    size_t h, dgu, xq, x_scale, hq, h_scale, arrived, partials, control, total;
 };
 bool ffn_shape_ok(const weave_ffn_config *c)
 {
@@ -205,8 +310,16 @@ FfnLayout ffn_layout(const weave_ffn_config *c)
     FfnLayout L;
     memset(&L, 0, sizeof(L));
     const size_t T = (size_t)c->max_tokens, H = (size_t)c->hidden, I = (size_t)c->ffn;
+    const long long step = c->weight_type == WEAVE_INT8 ? 128 : 64;
+    const long long up_tiles = (c->ffn + 127) / 128, down_tiles = (c->hidden + 255) / 256;
+    const long long up_units = up_tiles * ((c->hidden + step - 1) / step), down_units = down_tiles * ((c->ffn + step - 1) / step);
+    const StreamScratch s = stream_scratch(c->max_tokens, up_tiles > down_tiles ? up_tiles : down_tiles, up_units > down_units ? up_units : down_units);
     size_t at = up1024(sizeof(FfnCtl));
+    L.arrived = at;
+    at += up1024(s.arrived);
     L.control = at;
+    L.partials = at;
+    at += up1024(s.partials);
     L.h = at;
     at += up1024(T * I * 2);
     if (c->backward) {
@@ -235,6 +348,7 @@ struct weave_ffn {
     uint8_t *ws;
     CUtensorMap gate_k, up_k, down_k;          // K along the rows: forward products
     CUtensorMap gate_up_mn, down_mn;           // K across the rows: backward products
+    CUtensorMap gate_up_stream, down_stream;   // small batches
 };
 
 extern "C" {
@@ -266,6 +380,10 @@ int weave_ffn_create(const weave_ffn_config *cfg, weave_ffn_t *out)
         const uint8_t *up = static_cast<const uint8_t *>(cfg->gate_up) + (size_t)I * H * (i8 ? 1 : 2);
         bool ok = map_k(h->e, h->gate_k, type, cfg->gate_up, I, H) && map_k(h->e, h->up_k, type, up, I, H) &&
                   map_k(h->e, h->down_k, type, cfg->down, H, I);
+        ok = ok && map_stream_w(h->e, h->gate_up_stream, type, cfg->gate_up, I, H, true) &&
+             map_stream_w(h->e, h->down_stream, type, cfg->down, H, I, false);
+        h->e.arrived = reinterpret_cast<unsigned *>(h->ws + L.arrived);
+        h->e.partials = reinterpret_cast<uint32_t *>(h->ws + L.partials);
         if (cfg->backward) ok = ok && map_mn(h->e, h->gate_up_mn, cfg->gate_up, 2ll * I, H) && map_mn(h->e, h->down_mn, cfg->down, H, I);
         rc = ok ? engine_clear(h->e, L.control) : WEAVE_ERR_CUDA;
     }
@@ -290,40 +408,57 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     h->e.last_stream = stream;
     uint8_t *hbuf = h->ws + h->L.h;
-    cudaError_t err;
-    GemmArgs g, d;
-    if (h->cfg.weight_type == WEAVE_BF16) {
-        if (!map_k(h->e, g.a[0], WEAVE_BF16, x, T, H) || !map_2d(h->e, g.d[0], WEAVE_BF16, hbuf, T, I, 32, 64) ||
-            !map_k(h->e, d.a[0], WEAVE_BF16, hbuf, T, I) || !map_2d(h->e, d.d[0], WEAVE_BF16, out, T, H, 32, 64))
-            return WEAVE_ERR_CUDA;
-        g.b[0][0] = h->gate_k;
-        g.b[0][1] = h->up_k;
-        err = launch_gemm<kEpiGated, false, false, false>(h->e, g, T, I, H, 0, stream);
-        if (err != cudaSuccess) return cuda_fail(h->e, err);
-        d.b[0][0] = d.b[0][1] = h->down_k;
-        err = launch_gemm<kEpiStore, false, false, false>(h->e, d, T, H, I, 0, stream);
-        return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
-    }
     int8_t *xq = reinterpret_cast<int8_t *>(h->ws + h->L.xq), *hq = reinterpret_cast<int8_t *>(h->ws + h->L.hq);
     float *xs = reinterpret_cast<float *>(h->ws + h->L.x_scale), *hs = reinterpret_cast<float *>(h->ws + h->L.h_scale);
-    if (!map_k(h->e, g.a[0], WEAVE_INT8, xq, T, H) || !map_2d(h->e, g.d[0], WEAVE_BF16, hbuf, T, I, 32, 64) ||
-        !map_k(h->e, d.a[0], WEAVE_INT8, hq, T, I) || !map_2d(h->e, d.d[0], WEAVE_BF16, out, T, H, 32, 64))
+    const bool i8 = h->cfg.weight_type == WEAVE_INT8;
+    const int type = i8 ? WEAVE_INT8 : WEAVE_BF16;
+    const void *left = i8 ? static_cast<const void *>(xq) : x, *mid = i8 ? static_cast<const void *>(hq) : hbuf;
+    cudaError_t err = cudaSuccess;
+    if (use_stream(T)) {
+        FfnStreamArgs g, d;
+        if (!map_stream_x(h->e, g.x, type, left, T, H) || !map_stream_x(h->e, d.x, type, mid, T, I)) return WEAVE_ERR_CUDA;
+        g.w = h->gate_up_stream;
+        g.row_scale = xs;
+        g.col_scale = h->cfg.gate_up_scale;
+        g.out = hbuf;
+        g.out_f32 = 0;
+        d.w = h->down_stream;
+        d.row_scale = hs;
+        d.col_scale = h->cfg.down_scale;
+        d.out = out;
+        d.out_f32 = 0;
+        if (i8) {
+            err = launch_quant(x, WEAVE_BF16, T, H, xq, xs, false, stream);
+            if (err == cudaSuccess) err = launch_stream<true, true>(h->e, g, T, I, H, true, stream);
+            if (err == cudaSuccess) err = launch_quant(hbuf, WEAVE_BF16, T, I, hq, hs, true, stream);
+            if (err == cudaSuccess) err = launch_stream<true, false>(h->e, d, T, H, I, true, stream);
+        } else {
+            err = launch_stream<false, true>(h->e, g, T, I, H, false, stream);
+            if (err == cudaSuccess) err = launch_stream<false, false>(h->e, d, T, H, I, true, stream);
+        }
+        return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
+    }
+    GemmArgs g, d;
+    if (!map_k(h->e, g.a[0], type, left, T, H) || !map_2d(h->e, g.d[0], WEAVE_BF16, hbuf, T, I, 32, 64) ||
+        !map_k(h->e, d.a[0], type, mid, T, I) || !map_2d(h->e, d.d[0], WEAVE_BF16, out, T, H, 32, 64))
         return WEAVE_ERR_CUDA;
-    err = launch_quant(&h->e, x, WEAVE_BF16, T, H, xq, xs, stream);
-    if (err != cudaSuccess) return cuda_fail(h->e, err);
     g.b[0][0] = h->gate_k;
     g.b[0][1] = h->up_k;
     g.row_scale = xs;
     g.col_scale = h->cfg.gate_up_scale;
-    err = launch_gemm<kEpiScaledGated, true, false, false>(h->e, g, T, I, H, 0, stream);
-    if (err != cudaSuccess) return cuda_fail(h->e, err);
-    err = launch_quant(&h->e, hbuf, WEAVE_BF16, T, I, hq, hs, stream);
-    if (err != cudaSuccess) return cuda_fail(h->e, err);
     d.b[0][0] = d.b[0][1] = h->down_k;
     d.row_scale = hs;
     d.col_scale = h->cfg.down_scale;
     d.out_f32 = d.direct = 0;
-    err = launch_gemm<kEpiScaled, true, false, false>(h->e, d, T, H, I, 0, stream);
+    if (i8) {
+        err = launch_quant(x, WEAVE_BF16, T, H, xq, xs, false, stream);
+        if (err == cudaSuccess) err = launch_gemm<kEpiScaledGated, true, false, false>(h->e, g, T, I, H, 0, true, stream);
+        if (err == cudaSuccess) err = launch_quant(hbuf, WEAVE_BF16, T, I, hq, hs, true, stream);
+        if (err == cudaSuccess) err = launch_gemm<kEpiScaled, true, false, false>(h->e, d, T, H, I, 0, true, stream);
+    } else {
+        err = launch_gemm<kEpiGated, false, false, false>(h->e, g, T, I, H, 0, false, stream);
+        if (err == cudaSuccess) err = launch_gemm<kEpiStore, false, false, false>(h->e, d, T, H, I, 0, true, stream);
+    }
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }
 
@@ -361,25 +496,25 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     g.b[0][0] = g.b[0][1] = h->down_mn;
     g.b[1][0] = h->gate_k;
     g.b[1][1] = h->up_k;
-    err = launch_gemm<kEpiGrad, false, false, false>(h->e, g, T, I, H, H, stream);
+    err = launch_gemm<kEpiGrad, false, false, false>(h->e, g, T, I, H, H, false, stream);
     if (err != cudaSuccess) return cuda_fail(h->e, err);
     // dx = [dg du] W_gu
     if (!map_k(h->e, g.a[0], WEAVE_BF16, dgu, T, 2ll * I) || !map_2d(h->e, g.d[0], WEAVE_BF16, dx, T, H, 32, 64)) return WEAVE_ERR_CUDA;
     g.b[0][0] = g.b[0][1] = h->gate_up_mn;
-    err = launch_gemm<kEpiStore, false, false, true>(h->e, g, T, H, 2ll * I, 0, stream);
+    err = launch_gemm<kEpiStore, false, false, true>(h->e, g, T, H, 2ll * I, 0, true, stream);
     if (err != cudaSuccess) return cuda_fail(h->e, err);
     // dW_gu = [dg du]^T x
     if (!map_mn(h->e, g.a[0], dgu, T, 2ll * I) || !map_mn(h->e, g.b[0][0], x, T, H) ||
         !map_2d(h->e, g.d[0], WEAVE_BF16, dgate_up, 2ll * I, H, 32, 64))
         return WEAVE_ERR_CUDA;
     g.b[0][1] = g.b[0][0];
-    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, 2 * I, H, T, 0, stream);
+    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, 2 * I, H, T, 0, true, stream);
     if (err != cudaSuccess) return cuda_fail(h->e, err);
     // dW_d = dy^T h
     if (!map_mn(h->e, g.a[0], dy, T, H) || !map_mn(h->e, g.b[0][0], hbuf, T, I) || !map_2d(h->e, g.d[0], WEAVE_BF16, ddown, H, I, 32, 64))
         return WEAVE_ERR_CUDA;
     g.b[0][1] = g.b[0][0];
-    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, H, I, T, 0, stream);
+    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, H, I, T, 0, true, stream);
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }
 
@@ -405,7 +540,7 @@ int weave_ffn_destroy(weave_ffn_t h)
 // ------------------------------------------------------------------------------------ 8-bit integers
 
 namespace {
-struct Int8Layout { size_t xq, x_scale, control, total; };
+struct Int8Layout { size_t xq, x_scale, arrived, partials, control, total; };
 bool int8_shape_ok(const weave_int8_linear_config *c)
 {
     return c && c->in_features > 0 && c->in_features % 16 == 0 && c->in_features <= kMaxWidth && c->out_features > 0 &&
@@ -414,8 +549,14 @@ bool int8_shape_ok(const weave_int8_linear_config *c)
 Int8Layout int8_layout(const weave_int8_linear_config *c)
 {
     Int8Layout L;
+    const long long tiles = (c->out_features + 255ll) / 256;
+    const StreamScratch s = stream_scratch(c->max_tokens, tiles, tiles * ((c->in_features + 127) / 128));
     size_t at = up1024(sizeof(FfnCtl));
+    L.arrived = at;
+    at += up1024(s.arrived);
     L.control = at;
+    L.partials = at;
+    at += up1024(s.partials);
     L.xq = at;
     at += up1024((size_t)c->max_tokens * c->in_features);
     L.x_scale = at;
@@ -430,7 +571,7 @@ struct weave_int8_linear {
     weave_int8_linear_config cfg;
     Int8Layout L;
     uint8_t *ws;
-    CUtensorMap weight_k;
+    CUtensorMap weight_k, weight_stream;
 };
 
 extern "C" {
@@ -443,7 +584,7 @@ int weave_int8_quantize(const void *x, int x_type, int rows, int cols, void *q, 
     if (!x || !q || !scale || !aligned(x, size) || !aligned(scale, 4)) return WEAVE_ERR_INVALID_ARG;
     const Range outs[2] = {{q, n}, {scale, (size_t)rows * 4}}, ins[1] = {{x, n * size}};
     if (!outputs_clear(outs, 2, ins, 1)) return WEAVE_ERR_INVALID_ARG;
-    return launch_quant(nullptr, x, x_type, rows, cols, static_cast<int8_t *>(q), scale, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+    return launch_quant(x, x_type, rows, cols, static_cast<int8_t *>(q), scale, false, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
                ? WEAVE_OK
                : WEAVE_ERR_CUDA;
 }
@@ -467,9 +608,13 @@ int weave_int8_linear_create(const weave_int8_linear_config *cfg, weave_int8_lin
     h->L = L;
     h->ws = static_cast<uint8_t *>(cfg->workspace);
     int rc = engine_create(h->e, cfg->workspace);
-    if (rc == WEAVE_OK)
-        rc = map_k(h->e, h->weight_k, WEAVE_INT8, cfg->weight, cfg->out_features, cfg->in_features) ? engine_clear(h->e, L.control)
-                                                                                                    : WEAVE_ERR_CUDA;
+    if (rc == WEAVE_OK) {
+        h->e.arrived = reinterpret_cast<unsigned *>(h->ws + L.arrived);
+        h->e.partials = reinterpret_cast<uint32_t *>(h->ws + L.partials);
+        const bool ok = map_k(h->e, h->weight_k, WEAVE_INT8, cfg->weight, cfg->out_features, cfg->in_features) &&
+                        map_stream_w(h->e, h->weight_stream, WEAVE_INT8, cfg->weight, cfg->out_features, cfg->in_features, false);
+        rc = ok ? engine_clear(h->e, L.control) : WEAVE_ERR_CUDA;
+    }
     if (rc != WEAVE_OK) {
         delete h;
         return rc;
@@ -499,10 +644,22 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     if (x_type != WEAVE_INT8) {
         int8_t *xq = reinterpret_cast<int8_t *>(h->ws + h->L.xq);
         float *xs = reinterpret_cast<float *>(h->ws + h->L.x_scale);
-        err = launch_quant(&h->e, x, x_type, T, K, xq, xs, stream);
+        err = launch_quant(x, x_type, T, K, xq, xs, false, stream);
         if (err != cudaSuccess) return cuda_fail(h->e, err);
         q = xq;
         x_scale = xs;
+    }
+    const bool behind = x_type != WEAVE_INT8;
+    if (use_stream(T)) {
+        FfnStreamArgs g;
+        if (!map_stream_x(h->e, g.x, WEAVE_INT8, q, T, K)) return WEAVE_ERR_CUDA;
+        g.w = h->weight_stream;
+        g.row_scale = x_scale;
+        g.col_scale = h->cfg.scale;
+        g.out = out;
+        g.out_f32 = out_type == WEAVE_F32;
+        err = launch_stream<true, false>(h->e, g, T, N, K, behind, stream);
+        return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
     }
     GemmArgs g;
     g.direct = (size_t)N * out_size % 16 != 0;
@@ -514,7 +671,7 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     if (!map_k(h->e, g.a[0], WEAVE_INT8, q, T, K)) return WEAVE_ERR_CUDA;
     if (!g.direct && !map_2d(h->e, g.d[0], out_type, out, T, N, 32, out_type == WEAVE_F32 ? 32 : 64)) return WEAVE_ERR_CUDA;
     g.b[0][0] = g.b[0][1] = h->weight_k;
-    err = launch_gemm<kEpiScaled, true, false, false>(h->e, g, T, N, K, 0, stream);
+    err = launch_gemm<kEpiScaled, true, false, false>(h->e, g, T, N, K, 0, behind, stream);
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }
 

@@ -72,6 +72,12 @@ __device__ __forceinline__ void ffn_linger()
 
 // ------------------------------------------------------------------------------------ PTX forms the MoE kernels lack
 
+// Launches behind one another: a kernel that was launched as the programmatic dependent of the one before it in the
+// stream starts when all CTAs of that one have called the first function, and sees what it wrote behind the second.
+// Every kernel of a chain calls the second one, so that its end means the end of all before it.
+__device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // MN-major operand, 128-byte swizzle: boxes of 64 elements along MN by 64 of K.  Eight K rows (1024 bytes) are one
 // swizzle atom: stride byte offset = the next eight of K; leading byte offset = the next 64 along MN (the next box).
 __device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t smem_addr)
@@ -194,6 +200,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
     constexpr int kPhases = kEpi == kEpiGrad ? 2 : 1;
     constexpr int kStepK = kI8 ? 128 : 64;          // elements of K in a k-step
 
+    pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int i = 0; i < kGemmStages; ++i) { mbar_init(&bars.full[i], 1); mbar_init(&bars.empty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&bars.acc_full[i], 1); mbar_init(&bars.acc_empty[i], 8); }
@@ -211,6 +218,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
         // ---- producers: warp 0 brings this CTA's rows of A, warp 1 its part of B; all bytes of a stage are credited
         // to the full barrier in the pair's leader
         const bool load_a = warp == 0;
+        pdl_wait();
         int s = 0;
         uint32_t ph = 0;
         for (int t = pair; t < tiles && ok; t += pairs) {
@@ -292,6 +300,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
         const uint32_t stage = smem + kGemmSmemStaging + quarter * kGemmStaging;
         float *const scales = reinterpret_cast<float *>(smem_g + kGemmSmemScales + quarter * 256);
         const uint32_t empty0 = mapa_u32(smem_u32(&bars.acc_empty[0]), 0);
+        pdl_wait();
         int n = 0;
         uint32_t slot = 0;          // kEpiStore, kEpiScaled in bf16: half of the staging buffer that is written next
         for (int t = pair; t < tiles; t += pairs, ++n) {

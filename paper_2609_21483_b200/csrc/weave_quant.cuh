@@ -7,6 +7,7 @@
 #pragma once
 #include <cuda_bf16.h>
 #include <stdint.h>
+#include "weave_gemm.cuh"
 
 namespace weave {
 
@@ -65,6 +66,8 @@ __global__ void __launch_bounds__(kQuantThreads) weave_quant_kernel(const X *x, 
     constexpr bool kBf16 = sizeof(X) == 2;
     constexpr int kPer = 16 / sizeof(X);
     int flip = 0;
+    pdl_launch_dependents();
+    pdl_wait();
     for (long long row = blockIdx.x; row < rows; row += gridDim.x, flip ^= 1) {
         const X *src = x + row * cols;
         int8_t *dst = q + row * cols;
