@@ -17,7 +17,7 @@ _SRC_DIR = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libweave_moe.so")
 _UNITS = ["weave_moe.cu", "weave_ffn.cu"]
 _SOURCES = _UNITS + ["weave_kernel.cuh", "weave_stream.cuh", "weave_ptx.cuh", "weave_gemm.cuh",
-                     "weave_ffn_stream.cuh", "weave_quant.cuh"]
+                     "weave_ffn_small.cuh", "weave_quant.cuh"]
 _HEADERS = ["weave_moe.h", "weave_ffn.h"]
 
 WEAVE_OK = 0

@@ -7,7 +7,7 @@
 #include <string.h>
 #include <new>
 
-#include "weave_ffn_stream.cuh"
+#include "weave_ffn_small.cuh"
 #include "weave_gemm.cuh"
 #include "weave_quant.cuh"
 
@@ -32,8 +32,6 @@ struct Engine {
     cudaStream_t last_stream;
     int last_cuda_error;
     EncodeTiledFn encode;
-    unsigned *arrived;         // streaming kernel: arrivals per tile, and partial sums
-    uint32_t *partials;
 };
 
 int cuda_fail(Engine &e, cudaError_t err)
@@ -62,30 +60,16 @@ bool outputs_clear(const Range *out, int n_out, const Range *in, int n_in)
     return true;
 }
 
-// Scratch of the streaming kernel for the largest of a handle's products (N columns of the result, 128 of them in a
-// tile if they are gated).  Behind the control words, which creation clears.
-constexpr int kStreamCtas = 148;
-struct StreamScratch { size_t arrived, partials; };
-StreamScratch stream_scratch(int max_tokens, long long tiles, long long units)
-{
-    const long long T = max_tokens < kFfnStreamMaxT ? max_tokens : kFfnStreamMaxT;
-    const long long ctas = units < kStreamCtas ? units : kStreamCtas;
-    StreamScratch s;
-    s.arrived = (size_t)tiles * 4;
-    s.partials = (size_t)(2 * ctas * 256 * T * 4);
-    return s;
-}
-
 template <int kEpi, bool kI8, bool kAMn, bool kBMn>
 cudaError_t size_gemm()
 {
     return cudaFuncSetAttribute(weave_gemm_kernel<kEpi, kI8, kAMn, kBMn>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmemBytes);
 }
 
-template <bool kI8, bool kGated>
-cudaError_t size_stream()
+template <bool kI8>
+cudaError_t size_small()
 {
-    return cudaFuncSetAttribute(weave_ffn_stream_kernel<kI8, kGated>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFfnStreamSmem);
+    return cudaFuncSetAttribute(weave_ffn_small_kernel<kI8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmemMax);
 }
 
 int engine_create(Engine &e, void *workspace)
@@ -97,7 +81,7 @@ int engine_create(Engine &e, void *workspace)
         cudaDeviceGetAttribute(&smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, e.device) != cudaSuccess ||
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, e.device) != cudaSuccess)
         return WEAVE_ERR_CUDA;
-    if (major != 10 || smem < kGemmSmemBytes || sms < 2) return WEAVE_ERR_UNSUPPORTED_DEVICE;
+    if (major != 10 || smem < kSmallSmemMax || sms < 2) return WEAVE_ERR_UNSUPPORTED_DEVICE;
     e.n_sm = sms & ~1;
     e.ctl = static_cast<FfnCtl *>(workspace);
     e.timeout_ns = 4000ull * 1000000ull;
@@ -111,9 +95,8 @@ int engine_create(Engine &e, void *workspace)
     if ((err = size_gemm<kEpiStore, false, false, false>()) != cudaSuccess || (err = size_gemm<kEpiStore, false, false, true>()) != cudaSuccess ||
         (err = size_gemm<kEpiStore, false, true, true>()) != cudaSuccess || (err = size_gemm<kEpiGated, false, false, false>()) != cudaSuccess ||
         (err = size_gemm<kEpiGrad, false, false, false>()) != cudaSuccess || (err = size_gemm<kEpiScaled, true, false, false>()) != cudaSuccess ||
-        (err = size_gemm<kEpiScaledGated, true, false, false>()) != cudaSuccess || (err = size_stream<false, false>()) != cudaSuccess ||
-        (err = size_stream<false, true>()) != cudaSuccess || (err = size_stream<true, false>()) != cudaSuccess ||
-        (err = size_stream<true, true>()) != cudaSuccess)
+        (err = size_gemm<kEpiScaledGated, true, false, false>()) != cudaSuccess || (err = size_small<false>()) != cudaSuccess ||
+        (err = size_small<true>()) != cudaSuccess)
         return cuda_fail(e, err);
     return WEAVE_OK;
 }
@@ -166,97 +149,97 @@ bool map_k(const Engine &e, CUtensorMap &m, int type, const void *p, long long r
 {
     return map_2d(e, m, type, p, rows, cols, 128, type == WEAVE_INT8 ? 128 : 64);
 }
-// tokens' box of the streaming kernel (the N of its MMA)
-int stream_box(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
-bool map_stream_x(const Engine &e, CUtensorMap &m, int type, const void *p, int T, long long cols)
-{
-    return map_2d(e, m, type, p, T, cols, stream_box(T), type == WEAVE_INT8 ? 128 : 64);
-}
-// weights of the streaming kernel: 256 rows, or 128 rows of each of two halves of `rows` rows
-bool map_stream_w(const Engine &e, CUtensorMap &m, int type, const void *p, long long rows, long long cols, bool gated)
-{
-    if (!gated) return map_2d(e, m, type, p, rows, cols, 256, type == WEAVE_INT8 ? 128 : 64);
-    const int size = type == WEAVE_INT8 ? 1 : 2;
-    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, 2};
-    const cuuint64_t strides[2] = {(cuuint64_t)cols * size, (cuuint64_t)rows * cols * size};
-    const cuuint32_t box[3] = {(cuuint32_t)(128 / size), 128, 2}, ones[3] = {1, 1, 1};
-    return e.encode(&m, size == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides,
-                    box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 // operand whose K runs across the rows (bf16): 64 elements x 64 rows
 bool map_mn(const Engine &e, CUtensorMap &m, const void *p, long long rows, long long cols)
 {
     return map_2d(e, m, WEAVE_BF16, p, rows, cols, 64, 64);
 }
 
-#ifndef WEAVE_STREAM_T
-#define WEAVE_STREAM_T kFfnStreamMaxT
-#endif
-bool use_stream(int T) { return T <= WEAVE_STREAM_T; }
-
-// behind: launched while the launch before it in the stream, one of the same call, still runs (see pdl_wait())
+// kBehind: launched while the launch before it in the stream, one of the same call, still runs (see pdl_wait())
+enum LaunchKind { kPlain, kBehind, kCooperative };
 template <class... Params, class... Args>
-cudaError_t launch(void (*kernel)(Params...), int grid, int block, size_t smem, bool behind, cudaStream_t stream, const Args &...args)
+cudaError_t launch(void (*kernel)(Params...), int grid, int block, size_t smem, LaunchKind kind, cudaStream_t stream, const Args &...args)
 {
     cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
+    if (kind == kCooperative) {
+        at.id = cudaLaunchAttributeCooperative;
+        at.val.cooperative = 1;
+    } else {
+        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at.val.programmaticStreamSerializationAllowed = 1;
+    }
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3(grid);
     lc.blockDim = dim3(block);
     lc.dynamicSmemBytes = smem;
     lc.stream = stream;
     lc.attrs = &at;
-    lc.numAttrs = behind ? 1 : 0;
+    lc.numAttrs = kind == kPlain ? 0 : 1;
     return cudaLaunchKernelEx(&lc, kernel, args...);
 }
 
-// Units of work per CTA of the streaming kernel.  A CTA takes about 430 cycles per unit of 32 KB on its own and the
-// chip 10 cycles per unit in all; a shared tile costs its last CTA a round trip and the reading of 1 KB per segment and
-// token.
-int stream_units_per_cta(int T, int ksteps, int tiles, int ctas)
+// The first product of a, or the next one: its plan and its tensor maps.  x: what the product reads, [T][K].
+bool small_product(const Engine &e, SmallArgs &a, int type, const void *w, const void *x, int n, bool gated, int K, int T, const float *row_scale,
+                   const float *col_scale, void *out, bool out_f32)
 {
-    const long long units = (long long)ksteps * tiles;
-    const int least = (int)((units + ctas - 1) / ctas);
-    int best = least;
-    double best_cost = 1e30;
-    for (int u = least; u <= (least > ksteps ? least : ksteps); ++u) {
-        const int shared = u % ksteps == 0 ? 1 : ksteps % u == 0 ? ksteps / u : (ksteps + u - 1) / u + 1;
-        const double load = u * 430.0 > units * 10.0 ? u * 430.0 : units * 10.0;
-        const double cost = load + (shared > 1 ? 2500.0 + shared * (T * 16.0 + 50.0) : 0.0);
-        if (cost < best_cost) {
-            best_cost = cost;
-            best = u;
-        }
-    }
-    return best;
+    SmallProduct &p = a.p[a.products++];
+    const int size = type == WEAVE_INT8 ? 1 : 2, block = 128 / size;
+    p.s = small_shape(n, gated, K, block, T, e.n_sm);
+    p.gated = gated;
+    p.out_f32 = out_f32;
+    p.row_scale = row_scale;
+    p.col_scale = col_scale;
+    p.out = out;
+    p.round_src = nullptr;
+    p.K = K;
+    // with several blocks of K per step they are the maps' last dimension; with one, K is the first, clipped at its end
+    const bool blocks = p.s.kbs > 1;
+    const cuuint64_t row = (cuuint64_t)K * size, inner = blocks ? (cuuint64_t)block : (cuuint64_t)K, count = blocks ? (cuuint64_t)(K / block) : 1;
+    const cuuint64_t wd[4] = {inner, (cuuint64_t)n, gated ? 2u : 1u, count}, ws[3] = {row, row * (cuuint64_t)n, 128};
+    const cuuint32_t wb[4] = {(cuuint32_t)block, (cuuint32_t)p.s.ct, gated ? 2u : 1u, (cuuint32_t)p.s.kbs};
+    const cuuint64_t xd[3] = {inner, (cuuint64_t)T, count}, xs[2] = {row, 128};
+    const cuuint32_t xb[3] = {(cuuint32_t)block, (cuuint32_t)p.s.box_t, (cuuint32_t)p.s.kbs};
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    const CUtensorMapDataType dt = size == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    return e.encode(&p.w, dt, 4, const_cast<void *>(w), wd, ws, wb, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS &&
+           e.encode(&p.x, dt, 3, const_cast<void *>(x), xd, xs, xb, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// tokens that the kernel rounds to integers before the product made last
+void small_round(SmallArgs &a, const void *src, int src_type, int8_t *dst, float *scale)
+{
+    SmallProduct &p = a.p[a.products - 1];
+    p.round_src = src;
+    p.round_dst = dst;
+    p.round_scale = scale;
+    p.round_f32 = src_type == WEAVE_F32;
 }
 
-template <bool kI8, bool kGated>
-cudaError_t launch_stream(const Engine &e, FfnStreamArgs &a, int T, int N, long long K, bool behind, cudaStream_t stream)
+template <bool kI8>
+cudaError_t launch_small(const Engine &e, SmallArgs &a, int T, cudaStream_t stream)
 {
     a.ctl = e.ctl;
     a.timeout_ns = e.timeout_ns;
-    a.arrived = e.arrived;
-    a.partials = e.partials;
     a.T = T;
-    a.N = N;
-    a.ld_out = N;
-    a.ksteps = (int)((K + (kI8 ? 127 : 63)) / (kI8 ? 128 : 64));
-    a.tiles = (N + (kGated ? 127 : 255)) / (kGated ? 128 : 256);
-    a.units = a.ksteps * a.tiles;
-    const int ctas = e.n_sm < kStreamCtas ? e.n_sm : kStreamCtas;
-    a.units_per_cta = stream_units_per_cta(T, a.ksteps, a.tiles, ctas);
-    a.box_t = stream_box(T);
-    a.stages = ffn_stream_stages(a.box_t);
-    const size_t smem = 1024 + (size_t)a.stages * (kFfnStreamWeights + a.box_t * 128) + sizeof(FfnStreamBars);
-    return launch(weave_ffn_stream_kernel<kI8, kGated>, (a.units + a.units_per_cta - 1) / a.units_per_cta, kFfnStreamThreads, smem, behind,
-                  stream, a);
+    int w = 0, x = 0, cols = 16;
+    for (int i = 0; i < a.products; ++i) {
+        const SmallShape &s = a.p[i].s;
+        w = s.w_bytes > w ? s.w_bytes : w;
+        x = s.x_bytes > x ? s.x_bytes : x;
+        cols = s.kbs * s.box_t > cols ? s.kbs * s.box_t : cols;
+    }
+    a.x_offset = (int)up1024(w);
+    a.slot_bytes = a.x_offset + (int)up1024(x);
+    a.slots = kSmallMaxSlots;
+    while (small_smem_bytes(a.slots, a.slot_bytes) > kSmallSmemMax) --a.slots;
+    a.acc_cols = cols;
+    for (a.tmem_cols = 32; a.tmem_cols < 2 * cols;) a.tmem_cols *= 2;
+    return launch(weave_ffn_small_kernel<kI8>, e.n_sm, kSmallThreads, small_smem_bytes(a.slots, a.slot_bytes), kCooperative, stream, a);
 }
 
 template <int kEpi, bool kI8, bool kAMn, bool kBMn>
-cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int M, int N, long long K0, long long K1, bool behind, cudaStream_t stream)
+cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int M, int N, long long K0, long long K1, LaunchKind kind, cudaStream_t stream)
 {
     constexpr int tile_n = kEpi == kEpiStore || kEpi == kEpiScaled ? 256 : 128;
     constexpr int step = kI8 ? 128 : 64;
@@ -272,22 +255,29 @@ cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int M, int N, long long K0
     a.group_m = 8;
     const long long tiles = (long long)a.tiles_m * a.tiles_n;
     const int pairs = (int)(tiles < e.n_sm / 2 ? tiles : e.n_sm / 2);
-    return launch(weave_gemm_kernel<kEpi, kI8, kAMn, kBMn>, pairs * 2, kGemmThreads, kGemmSmemBytes, behind, stream, a);
+    return launch(weave_gemm_kernel<kEpi, kI8, kAMn, kBMn>, pairs * 2, kGemmThreads, kGemmSmemBytes, kind, stream, a);
 }
 
-cudaError_t launch_quant(const void *x, int type, int rows, int cols, int8_t *q, float *scale, bool behind, cudaStream_t stream)
+template <class X, int kThreads>
+cudaError_t launch_quant_as(const void *x, int rows, int cols, int8_t *q, float *scale, LaunchKind kind, cudaStream_t stream)
 {
-    const int grid = rows < 148 * 8 ? rows : 148 * 8;
-    const bool vec = (long long)cols * (type == WEAVE_BF16 ? 2 : 4) % 16 == 0 && aligned(x, 16) && aligned(q, 16);
-    const long long r = rows, c = cols;
-    if (type == WEAVE_BF16) {
-        const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(x);
-        return launch(vec ? weave_quant_kernel<__nv_bfloat16, true> : weave_quant_kernel<__nv_bfloat16, false>, grid, kQuantThreads, 0, behind,
-                      stream, p, q, scale, r, c);
-    }
-    const float *p = static_cast<const float *>(x);
-    return launch(vec ? weave_quant_kernel<float, true> : weave_quant_kernel<float, false>, grid, kQuantThreads, 0, behind, stream, p, q, scale,
-                  r, c);
+    const bool vec = (long long)cols * (int)sizeof(X) % 16 == 0 && aligned(x, 16) && aligned(q, 16);
+    return launch(vec ? weave_quant_kernel<X, kThreads, true> : weave_quant_kernel<X, kThreads, false>, rows, kThreads, 0, kind, stream,
+                  static_cast<const X *>(x), q, scale, cols);
+}
+template <class X>
+cudaError_t launch_quant_rows(const void *x, int rows, int cols, int8_t *q, float *scale, LaunchKind kind, cudaStream_t stream)
+{
+    // threads with four to eight vectors each; few rows get many threads
+    const int vectors = cols / (int)(16 / sizeof(X));
+    if (vectors <= 512 && rows >= 1024) return launch_quant_as<X, 64>(x, rows, cols, q, scale, kind, stream);
+    if (vectors <= 1024 && rows >= 512) return launch_quant_as<X, 128>(x, rows, cols, q, scale, kind, stream);
+    return launch_quant_as<X, 256>(x, rows, cols, q, scale, kind, stream);
+}
+cudaError_t launch_quant(const void *x, int type, int rows, int cols, int8_t *q, float *scale, LaunchKind kind, cudaStream_t stream)
+{
+    return type == WEAVE_BF16 ? launch_quant_rows<__nv_bfloat16>(x, rows, cols, q, scale, kind, stream)
+                              : launch_quant_rows<float>(x, rows, cols, q, scale, kind, stream);
 }
 
 }  // namespace
@@ -296,7 +286,7 @@ cudaError_t launch_quant(const void *x, int type, int rows, int cols, int8_t *q,
 
 namespace {
 struct FfnLayout {
-    size_t h, dgu, xq, x_scale, hq, h_scale, arrived, partials, control, total;
+    size_t h, dgu, xq, x_scale, hq, h_scale, control, total;
 };
 bool ffn_shape_ok(const weave_ffn_config *c)
 {
@@ -310,16 +300,8 @@ FfnLayout ffn_layout(const weave_ffn_config *c)
     FfnLayout L;
     memset(&L, 0, sizeof(L));
     const size_t T = (size_t)c->max_tokens, H = (size_t)c->hidden, I = (size_t)c->ffn;
-    const long long step = c->weight_type == WEAVE_INT8 ? 128 : 64;
-    const long long up_tiles = (c->ffn + 127) / 128, down_tiles = (c->hidden + 255) / 256;
-    const long long up_units = up_tiles * ((c->hidden + step - 1) / step), down_units = down_tiles * ((c->ffn + step - 1) / step);
-    const StreamScratch s = stream_scratch(c->max_tokens, up_tiles > down_tiles ? up_tiles : down_tiles, up_units > down_units ? up_units : down_units);
     size_t at = up1024(sizeof(FfnCtl));
-    L.arrived = at;
-    at += up1024(s.arrived);
     L.control = at;
-    L.partials = at;
-    at += up1024(s.partials);
     L.h = at;
     at += up1024(T * I * 2);
     if (c->backward) {
@@ -348,7 +330,6 @@ struct weave_ffn {
     uint8_t *ws;
     CUtensorMap gate_k, up_k, down_k;          // K along the rows: forward products
     CUtensorMap gate_up_mn, down_mn;           // K across the rows: backward products
-    CUtensorMap gate_up_stream, down_stream;   // small batches
 };
 
 extern "C" {
@@ -380,10 +361,6 @@ int weave_ffn_create(const weave_ffn_config *cfg, weave_ffn_t *out)
         const uint8_t *up = static_cast<const uint8_t *>(cfg->gate_up) + (size_t)I * H * (i8 ? 1 : 2);
         bool ok = map_k(h->e, h->gate_k, type, cfg->gate_up, I, H) && map_k(h->e, h->up_k, type, up, I, H) &&
                   map_k(h->e, h->down_k, type, cfg->down, H, I);
-        ok = ok && map_stream_w(h->e, h->gate_up_stream, type, cfg->gate_up, I, H, true) &&
-             map_stream_w(h->e, h->down_stream, type, cfg->down, H, I, false);
-        h->e.arrived = reinterpret_cast<unsigned *>(h->ws + L.arrived);
-        h->e.partials = reinterpret_cast<uint32_t *>(h->ws + L.partials);
         if (cfg->backward) ok = ok && map_mn(h->e, h->gate_up_mn, cfg->gate_up, 2ll * I, H) && map_mn(h->e, h->down_mn, cfg->down, H, I);
         rc = ok ? engine_clear(h->e, L.control) : WEAVE_ERR_CUDA;
     }
@@ -414,28 +391,14 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     const int type = i8 ? WEAVE_INT8 : WEAVE_BF16;
     const void *left = i8 ? static_cast<const void *>(xq) : x, *mid = i8 ? static_cast<const void *>(hq) : hbuf;
     cudaError_t err = cudaSuccess;
-    if (use_stream(T)) {
-        FfnStreamArgs g, d;
-        if (!map_stream_x(h->e, g.x, type, left, T, H) || !map_stream_x(h->e, d.x, type, mid, T, I)) return WEAVE_ERR_CUDA;
-        g.w = h->gate_up_stream;
-        g.row_scale = xs;
-        g.col_scale = h->cfg.gate_up_scale;
-        g.out = hbuf;
-        g.out_f32 = 0;
-        d.w = h->down_stream;
-        d.row_scale = hs;
-        d.col_scale = h->cfg.down_scale;
-        d.out = out;
-        d.out_f32 = 0;
-        if (i8) {
-            err = launch_quant(x, WEAVE_BF16, T, H, xq, xs, false, stream);
-            if (err == cudaSuccess) err = launch_stream<true, true>(h->e, g, T, I, H, true, stream);
-            if (err == cudaSuccess) err = launch_quant(hbuf, WEAVE_BF16, T, I, hq, hs, true, stream);
-            if (err == cudaSuccess) err = launch_stream<true, false>(h->e, d, T, H, I, true, stream);
-        } else {
-            err = launch_stream<false, true>(h->e, g, T, I, H, false, stream);
-            if (err == cudaSuccess) err = launch_stream<false, false>(h->e, d, T, H, I, true, stream);
-        }
+    if (T <= kSmallMaxT) {
+        SmallArgs a;
+        a.products = 0;
+        if (!small_product(h->e, a, type, h->cfg.gate_up, left, I, true, H, T, xs, h->cfg.gate_up_scale, hbuf, false)) return WEAVE_ERR_CUDA;
+        if (i8) small_round(a, x, WEAVE_BF16, xq, xs);
+        if (!small_product(h->e, a, type, h->cfg.down, mid, H, false, I, T, hs, h->cfg.down_scale, out, false)) return WEAVE_ERR_CUDA;
+        if (i8) small_round(a, hbuf, WEAVE_BF16, hq, hs);
+        err = i8 ? launch_small<true>(h->e, a, T, stream) : launch_small<false>(h->e, a, T, stream);
         return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
     }
     GemmArgs g, d;
@@ -451,13 +414,13 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     d.col_scale = h->cfg.down_scale;
     d.out_f32 = d.direct = 0;
     if (i8) {
-        err = launch_quant(x, WEAVE_BF16, T, H, xq, xs, false, stream);
-        if (err == cudaSuccess) err = launch_gemm<kEpiScaledGated, true, false, false>(h->e, g, T, I, H, 0, true, stream);
-        if (err == cudaSuccess) err = launch_quant(hbuf, WEAVE_BF16, T, I, hq, hs, true, stream);
-        if (err == cudaSuccess) err = launch_gemm<kEpiScaled, true, false, false>(h->e, d, T, H, I, 0, true, stream);
+        err = launch_quant(x, WEAVE_BF16, T, H, xq, xs, kPlain, stream);
+        if (err == cudaSuccess) err = launch_gemm<kEpiScaledGated, true, false, false>(h->e, g, T, I, H, 0, kBehind, stream);
+        if (err == cudaSuccess) err = launch_quant(hbuf, WEAVE_BF16, T, I, hq, hs, kBehind, stream);
+        if (err == cudaSuccess) err = launch_gemm<kEpiScaled, true, false, false>(h->e, d, T, H, I, 0, kBehind, stream);
     } else {
-        err = launch_gemm<kEpiGated, false, false, false>(h->e, g, T, I, H, 0, false, stream);
-        if (err == cudaSuccess) err = launch_gemm<kEpiStore, false, false, false>(h->e, d, T, H, I, 0, true, stream);
+        err = launch_gemm<kEpiGated, false, false, false>(h->e, g, T, I, H, 0, kPlain, stream);
+        if (err == cudaSuccess) err = launch_gemm<kEpiStore, false, false, false>(h->e, d, T, H, I, 0, kBehind, stream);
     }
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }
@@ -496,25 +459,25 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     g.b[0][0] = g.b[0][1] = h->down_mn;
     g.b[1][0] = h->gate_k;
     g.b[1][1] = h->up_k;
-    err = launch_gemm<kEpiGrad, false, false, false>(h->e, g, T, I, H, H, false, stream);
+    err = launch_gemm<kEpiGrad, false, false, false>(h->e, g, T, I, H, H, kPlain, stream);
     if (err != cudaSuccess) return cuda_fail(h->e, err);
     // dx = [dg du] W_gu
     if (!map_k(h->e, g.a[0], WEAVE_BF16, dgu, T, 2ll * I) || !map_2d(h->e, g.d[0], WEAVE_BF16, dx, T, H, 32, 64)) return WEAVE_ERR_CUDA;
     g.b[0][0] = g.b[0][1] = h->gate_up_mn;
-    err = launch_gemm<kEpiStore, false, false, true>(h->e, g, T, H, 2ll * I, 0, true, stream);
+    err = launch_gemm<kEpiStore, false, false, true>(h->e, g, T, H, 2ll * I, 0, kBehind, stream);
     if (err != cudaSuccess) return cuda_fail(h->e, err);
     // dW_gu = [dg du]^T x
     if (!map_mn(h->e, g.a[0], dgu, T, 2ll * I) || !map_mn(h->e, g.b[0][0], x, T, H) ||
         !map_2d(h->e, g.d[0], WEAVE_BF16, dgate_up, 2ll * I, H, 32, 64))
         return WEAVE_ERR_CUDA;
     g.b[0][1] = g.b[0][0];
-    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, 2 * I, H, T, 0, true, stream);
+    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, 2 * I, H, T, 0, kBehind, stream);
     if (err != cudaSuccess) return cuda_fail(h->e, err);
     // dW_d = dy^T h
     if (!map_mn(h->e, g.a[0], dy, T, H) || !map_mn(h->e, g.b[0][0], hbuf, T, I) || !map_2d(h->e, g.d[0], WEAVE_BF16, ddown, H, I, 32, 64))
         return WEAVE_ERR_CUDA;
     g.b[0][1] = g.b[0][0];
-    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, H, I, T, 0, true, stream);
+    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, H, I, T, 0, kBehind, stream);
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }
 
@@ -540,7 +503,7 @@ int weave_ffn_destroy(weave_ffn_t h)
 // ------------------------------------------------------------------------------------ 8-bit integers
 
 namespace {
-struct Int8Layout { size_t xq, x_scale, arrived, partials, control, total; };
+struct Int8Layout { size_t xq, x_scale, control, total; };
 bool int8_shape_ok(const weave_int8_linear_config *c)
 {
     return c && c->in_features > 0 && c->in_features % 16 == 0 && c->in_features <= kMaxWidth && c->out_features > 0 &&
@@ -549,14 +512,8 @@ bool int8_shape_ok(const weave_int8_linear_config *c)
 Int8Layout int8_layout(const weave_int8_linear_config *c)
 {
     Int8Layout L;
-    const long long tiles = (c->out_features + 255ll) / 256;
-    const StreamScratch s = stream_scratch(c->max_tokens, tiles, tiles * ((c->in_features + 127) / 128));
     size_t at = up1024(sizeof(FfnCtl));
-    L.arrived = at;
-    at += up1024(s.arrived);
     L.control = at;
-    L.partials = at;
-    at += up1024(s.partials);
     L.xq = at;
     at += up1024((size_t)c->max_tokens * c->in_features);
     L.x_scale = at;
@@ -571,7 +528,7 @@ struct weave_int8_linear {
     weave_int8_linear_config cfg;
     Int8Layout L;
     uint8_t *ws;
-    CUtensorMap weight_k, weight_stream;
+    CUtensorMap weight_k;
 };
 
 extern "C" {
@@ -584,7 +541,7 @@ int weave_int8_quantize(const void *x, int x_type, int rows, int cols, void *q, 
     if (!x || !q || !scale || !aligned(x, size) || !aligned(scale, 4)) return WEAVE_ERR_INVALID_ARG;
     const Range outs[2] = {{q, n}, {scale, (size_t)rows * 4}}, ins[1] = {{x, n * size}};
     if (!outputs_clear(outs, 2, ins, 1)) return WEAVE_ERR_INVALID_ARG;
-    return launch_quant(x, x_type, rows, cols, static_cast<int8_t *>(q), scale, false, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
+    return launch_quant(x, x_type, rows, cols, static_cast<int8_t *>(q), scale, kPlain, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
                ? WEAVE_OK
                : WEAVE_ERR_CUDA;
 }
@@ -608,13 +565,9 @@ int weave_int8_linear_create(const weave_int8_linear_config *cfg, weave_int8_lin
     h->L = L;
     h->ws = static_cast<uint8_t *>(cfg->workspace);
     int rc = engine_create(h->e, cfg->workspace);
-    if (rc == WEAVE_OK) {
-        h->e.arrived = reinterpret_cast<unsigned *>(h->ws + L.arrived);
-        h->e.partials = reinterpret_cast<uint32_t *>(h->ws + L.partials);
-        const bool ok = map_k(h->e, h->weight_k, WEAVE_INT8, cfg->weight, cfg->out_features, cfg->in_features) &&
-                        map_stream_w(h->e, h->weight_stream, WEAVE_INT8, cfg->weight, cfg->out_features, cfg->in_features, false);
-        rc = ok ? engine_clear(h->e, L.control) : WEAVE_ERR_CUDA;
-    }
+    if (rc == WEAVE_OK)
+        rc = map_k(h->e, h->weight_k, WEAVE_INT8, cfg->weight, cfg->out_features, cfg->in_features) ? engine_clear(h->e, L.control)
+                                                                                                    : WEAVE_ERR_CUDA;
     if (rc != WEAVE_OK) {
         delete h;
         return rc;
@@ -639,27 +592,24 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     if (!outputs_clear(outs, 1, ins, 5) || !on_its_device(h->e)) return WEAVE_ERR_INVALID_ARG;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     h->e.last_stream = stream;
-    const void *q = x;
     cudaError_t err;
-    if (x_type != WEAVE_INT8) {
-        int8_t *xq = reinterpret_cast<int8_t *>(h->ws + h->L.xq);
-        float *xs = reinterpret_cast<float *>(h->ws + h->L.x_scale);
-        err = launch_quant(x, x_type, T, K, xq, xs, false, stream);
-        if (err != cudaSuccess) return cuda_fail(h->e, err);
-        q = xq;
-        x_scale = xs;
-    }
-    const bool behind = x_type != WEAVE_INT8;
-    if (use_stream(T)) {
-        FfnStreamArgs g;
-        if (!map_stream_x(h->e, g.x, WEAVE_INT8, q, T, K)) return WEAVE_ERR_CUDA;
-        g.w = h->weight_stream;
-        g.row_scale = x_scale;
-        g.col_scale = h->cfg.scale;
-        g.out = out;
-        g.out_f32 = out_type == WEAVE_F32;
-        err = launch_stream<true, false>(h->e, g, T, N, K, behind, stream);
+    int8_t *xq = reinterpret_cast<int8_t *>(h->ws + h->L.xq);
+    float *xs = reinterpret_cast<float *>(h->ws + h->L.x_scale);
+    const bool round = x_type != WEAVE_INT8;
+    const void *q = round ? xq : x;
+    if (round) x_scale = xs;
+    if (T <= kSmallMaxT) {
+        SmallArgs a;
+        a.products = 0;
+        if (!small_product(h->e, a, WEAVE_INT8, h->cfg.weight, q, N, false, K, T, x_scale, h->cfg.scale, out, out_type == WEAVE_F32))
+            return WEAVE_ERR_CUDA;
+        if (round) small_round(a, x, x_type, xq, xs);
+        err = launch_small<true>(h->e, a, T, stream);
         return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
+    }
+    if (round) {
+        err = launch_quant(x, x_type, T, K, xq, xs, kPlain, stream);
+        if (err != cudaSuccess) return cuda_fail(h->e, err);
     }
     GemmArgs g;
     g.direct = (size_t)N * out_size % 16 != 0;
@@ -671,7 +621,7 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     if (!map_k(h->e, g.a[0], WEAVE_INT8, q, T, K)) return WEAVE_ERR_CUDA;
     if (!g.direct && !map_2d(h->e, g.d[0], out_type, out, T, N, 32, out_type == WEAVE_F32 ? 32 : 64)) return WEAVE_ERR_CUDA;
     g.b[0][0] = g.b[0][1] = h->weight_k;
-    err = launch_gemm<kEpiScaled, true, false, false>(h->e, g, T, N, K, 0, behind, stream);
+    err = launch_gemm<kEpiScaled, true, false, false>(h->e, g, T, N, K, 0, round ? kBehind : kPlain, stream);
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }
 

@@ -26,7 +26,8 @@ enum { kEpiStore = 0, kEpiGated = 1, kEpiGrad = 2, kEpiScaled = 3, kEpiScaledGat
 struct FfnCtl {
     int status;          // 0 or the error that the first failed wait recorded
     int where;           // which wait that was
-    unsigned pad[62];
+    unsigned pad[30];
+    unsigned long long barrier[16];      // grid barriers of the small batches' kernel: arrivals since creation
 };
 static_assert(sizeof(FfnCtl) == 256, "the workspace layout counts on it");
 

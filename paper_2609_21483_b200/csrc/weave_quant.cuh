@@ -3,7 +3,8 @@
 // tie, or within a rounding of one, for about one value in a thousand, and a quotient rounded to fp32 would decide
 // those by its own rounding.
 //
-// Bound: HBM (3 bytes per bf16 value).  One block per row, the row kept in registers between the two passes over it.
+// Bound: HBM (3 bytes per bf16 value).  A row is read once: its threads keep it in registers (up to eight 16-byte
+// vectors each) between the search for the largest magnitude and the rounding.
 #pragma once
 #include <cuda_bf16.h>
 #include <stdint.h>
@@ -11,39 +12,43 @@
 
 namespace weave {
 
-constexpr int kQuantThreads = 256;
 constexpr int kQuantKeep = 8;          // 16-byte vectors of a row that a thread keeps
+constexpr float kQuantMagic = 12582912.0f;      // 1.5 * 2^23: adding it rounds to an integer, in the low bits of the sum
 
 struct QuantRow {
     float k, s, inv, half;             // x and the scale are multiplied by k (a power of two, exact) so that 1 / s is finite
     bool zero;                         // nothing but zeros: an all-zero row, or one with inf or NaN in it
 };
 
-// t is within one of the quotient; the remainder d = x - t s is exact (a multiple of half an ulp of s below s), so
-// comparing it with s / 2 decides the rounding
-__device__ __forceinline__ int quant_one(float x, const QuantRow &r)
+// The sum's low byte is the integer; it may be one off next to a tie, which the remainder shows: d = x - t s is exact
+// (a multiple of half an ulp of s, below s).
+__device__ __forceinline__ uint32_t quant_guess(float x, const QuantRow &r, bool &close)
 {
     const float y = x * r.k;
-    float t = rintf(y * r.inv);
+    const float m = fmaf(y, r.inv, kQuantMagic);
+    close |= fabsf(fmaf(kQuantMagic - m, r.s, y)) >= r.half;
+    return __float_as_uint(m);
+}
+__device__ __noinline__ uint32_t quant_decide(float x, QuantRow r)
+{
+    const float y = x * r.k;
+    float t = fmaf(y, r.inv, kQuantMagic) - kQuantMagic;
     const float d = fmaf(-t, r.s, y);
-    if (fabsf(d) >= r.half) {
-        if (fabsf(d) > r.half || ((int)t & 1)) t += d > 0.0f ? 1.0f : -1.0f;
-        t = fminf(fmaxf(t, -127.0f), 127.0f);        // only rows whose scale is a denormal number reach beyond
-    }
-    return (int)t;
+    if (fabsf(d) > r.half || (fabsf(d) == r.half && ((int)t & 1))) t += d > 0.0f ? 1.0f : -1.0f;
+    return (uint32_t)(int)fminf(fmaxf(t, -127.0f), 127.0f);        // only rows whose scale is a denormal number reach beyond
 }
 __device__ __forceinline__ uint32_t quant_four(float a, float b, float c, float d, const QuantRow &r)
 {
     if (r.zero) return 0u;
-    return (uint32_t)(quant_one(a, r) & 255) | (uint32_t)(quant_one(b, r) & 255) << 8 | (uint32_t)(quant_one(c, r) & 255) << 16 |
-           (uint32_t)quant_one(d, r) << 24;
-}
-
-// the largest |x| as bits: NaN above inf above every number, so that either shows in the result
-__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
-__device__ __forceinline__ uint32_t abs_bits_bf16x2(uint32_t u)
-{
-    return max((u << 16) & 0x7FFFFFFFu, u & 0x7FFF0000u);
+    bool close = r.k != 1.0f;
+    uint32_t v[4] = {quant_guess(a, r, close), quant_guess(b, r, close), quant_guess(c, r, close), quant_guess(d, r, close)};
+    if (close) {
+        v[0] = quant_decide(a, r);
+        v[1] = quant_decide(b, r);
+        v[2] = quant_decide(c, r);
+        v[3] = quant_decide(d, r);
+    }
+    return __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
 }
 
 __device__ __forceinline__ QuantRow quant_row(uint32_t amax_bits, float &scale)
@@ -58,74 +63,87 @@ __device__ __forceinline__ QuantRow quant_row(uint32_t amax_bits, float &scale)
     return r;
 }
 
-// kVec: rows start on 16-byte boundaries and are whole 16-byte vectors long
-template <typename X, bool kVec>
-__global__ void __launch_bounds__(kQuantThreads) weave_quant_kernel(const X *x, int8_t *q, float *scale, long long rows, long long cols)
+// the largest magnitudes as bits: NaN above inf above every number, so that either shows in the result
+template <class X>
+__device__ __forceinline__ uint32_t quant_max(uint32_t m, const uint4 &v)
 {
-    __shared__ uint32_t warp_max[2][kQuantThreads / 32];
-    constexpr bool kBf16 = sizeof(X) == 2;
-    constexpr int kPer = 16 / sizeof(X);
-    int flip = 0;
-    pdl_launch_dependents();
-    pdl_wait();
-    for (long long row = blockIdx.x; row < rows; row += gridDim.x, flip ^= 1) {
-        const X *src = x + row * cols;
-        int8_t *dst = q + row * cols;
-        uint32_t m = 0;
-        uint4 keep[kQuantKeep];
-        const long long nv = cols / kPer;
-        if constexpr (kVec) {
-            auto max_of = [&](const uint4 &v) {
-                if constexpr (kBf16)
-                    m = max(m, max(max(abs_bits_bf16x2(v.x), abs_bits_bf16x2(v.y)), max(abs_bits_bf16x2(v.z), abs_bits_bf16x2(v.w))));
-                else
-                    m = max(m, max(max(v.x & 0x7FFFFFFFu, v.y & 0x7FFFFFFFu), max(v.z & 0x7FFFFFFFu, v.w & 0x7FFFFFFFu)));
-            };
+    if constexpr (sizeof(X) == 2) {      // two maxima, one per half
+        m = __vmaxu2(__vmaxu2(m, v.x & 0x7FFF7FFFu), v.y & 0x7FFF7FFFu);
+        return __vmaxu2(__vmaxu2(m, v.z & 0x7FFF7FFFu), v.w & 0x7FFF7FFFu);
+    } else {
+        m = max(max(m, v.x & 0x7FFFFFFFu), v.y & 0x7FFFFFFFu);
+        return max(max(m, v.z & 0x7FFFFFFFu), v.w & 0x7FFFFFFFu);
+    }
+}
+template <class X>
+__device__ __forceinline__ void quant_put(int8_t *dst, int at, const uint4 &v, const QuantRow &r)
+{
+    if constexpr (sizeof(X) == 2) {
+        const uint32_t lo = quant_four(bf16lo_to_f32(v.x), bf16hi_to_f32(v.x), bf16lo_to_f32(v.y), bf16hi_to_f32(v.y), r);
+        const uint32_t hi = quant_four(bf16lo_to_f32(v.z), bf16hi_to_f32(v.z), bf16lo_to_f32(v.w), bf16hi_to_f32(v.w), r);
+        reinterpret_cast<uint2 *>(dst)[at] = make_uint2(lo, hi);
+    } else {
+        reinterpret_cast<uint32_t *>(dst)[at] =
+            quant_four(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w), r);
+    }
+}
+
+// One row by kThreads threads (tid from 0), which meet at __syncthreads() or, kNamed, at named barrier 1.  kVec: rows
+// start on 16-byte boundaries and are whole 16-byte vectors long.  `part`: one word of shared memory per warp.  The row
+// is read past L1, as another SM may just have written it.
+template <class X, int kThreads, bool kVec, bool kNamed>
+__device__ __forceinline__ void quant_row_by(const X *x, int8_t *q, float *scale, long long row, int cols, int tid, uint32_t *part)
+{
+    const X *src = x + row * cols;
+    int8_t *dst = q + row * cols;
+    const uint4 *vec = reinterpret_cast<const uint4 *>(src);
+    const int nv = cols / (int)(16 / sizeof(X));
+    uint32_t m = 0;
+    uint4 keep[kQuantKeep];
+    if constexpr (kVec) {
 #pragma unroll
-            for (int i = 0; i < kQuantKeep; ++i) {
-                const long long at = threadIdx.x + (long long)i * kQuantThreads;
-                keep[i] = at < nv ? reinterpret_cast<const uint4 *>(src)[at] : make_uint4(0, 0, 0, 0);
-            }
+        for (int i = 0; i < kQuantKeep; ++i) keep[i] = tid + i * kThreads < nv ? __ldcg(vec + tid + i * kThreads) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < kQuantKeep; ++i) max_of(keep[i]);
-            for (long long at = threadIdx.x + (long long)kQuantKeep * kQuantThreads; at < nv; at += kQuantThreads)
-                max_of(reinterpret_cast<const uint4 *>(src)[at]);
-        } else {
-            for (long long at = threadIdx.x; at < cols; at += kQuantThreads) m = max(m, abs_bits((float)src[at]));
-        }
-        m = __reduce_max_sync(0xffffffffu, m);
-        if ((threadIdx.x & 31) == 0) warp_max[flip][threadIdx.x >> 5] = m;
-        __syncthreads();
-        m = 0;
+        for (int i = 0; i < kQuantKeep; ++i) m = quant_max<X>(m, keep[i]);
+        for (int at = tid + kQuantKeep * kThreads; at < nv; at += kThreads) m = quant_max<X>(m, __ldcg(vec + at));
+        if constexpr (sizeof(X) == 2) m = max(m << 16, m & 0xFFFF0000u);
+    } else {
+        for (int at = tid; at < cols; at += kThreads) m = max(m, __float_as_uint((float)src[at]) & 0x7FFFFFFFu);
+    }
+    m = __reduce_max_sync(0xffffffffu, m);
+    if constexpr (kThreads > 32) {
+        if ((tid & 31) == 0) part[tid >> 5] = m;
+        if constexpr (kNamed) named_barrier_sync<1, kThreads>();
+        else __syncthreads();
+        m = part[0];
 #pragma unroll
-        for (int w = 0; w < kQuantThreads / 32; ++w) m = max(m, warp_max[flip][w]);
-        float s;
-        const QuantRow r = quant_row(m, s);
-        if (threadIdx.x == 0) scale[row] = s;
-        if constexpr (kVec) {
-            auto put = [&](const uint4 &v, long long at) {
-                if constexpr (kBf16) {
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-                    float f[8];
+        for (int w = 1; w < kThreads / 32; ++w) m = max(m, part[w]);
+        // (a second row needs another barrier before it writes `part`: callers have one)
+    }
+    float s;
+    const QuantRow r = quant_row(m, s);
+    if (tid == 0) scale[row] = s;
+    if constexpr (kVec) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-                    reinterpret_cast<uint2 *>(dst)[at] = make_uint2(quant_four(f[0], f[1], f[2], f[3], r), quant_four(f[4], f[5], f[6], f[7], r));
-                } else {
-                    reinterpret_cast<uint32_t *>(dst)[at] =
-                        quant_four(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w), r);
-                }
-            };
-#pragma unroll
-            for (int i = 0; i < kQuantKeep; ++i) {
-                const long long at = threadIdx.x + (long long)i * kQuantThreads;
-                if (at < nv) put(keep[i], at);
-            }
-            for (long long at = threadIdx.x + (long long)kQuantKeep * kQuantThreads; at < nv; at += kQuantThreads)
-                put(reinterpret_cast<const uint4 *>(src)[at], at);
-        } else {
-            for (long long at = threadIdx.x; at < cols; at += kQuantThreads) dst[at] = r.zero ? 0 : (int8_t)quant_one((float)src[at], r);
+        for (int i = 0; i < kQuantKeep; ++i)
+            if (tid + i * kThreads < nv) quant_put<X>(dst, tid + i * kThreads, keep[i], r);
+        for (int at = tid + kQuantKeep * kThreads; at < nv; at += kThreads) quant_put<X>(dst, at, __ldcg(vec + at), r);
+    } else {
+        for (int at = tid; at < cols; at += kThreads) {
+            const float v = (float)src[at];
+            dst[at] = r.zero ? 0 : (int8_t)quant_decide(v, r);
         }
     }
+}
+
+// one row per block
+template <class X, int kThreads, bool kVec>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) weave_quant_kernel(const X *x, int8_t *q, float *scale, int cols)
+{
+    __shared__ uint32_t part[kThreads / 32];
+    pdl_launch_dependents();
+    pdl_wait();
+    quant_row_by<X, kThreads, kVec, false>(x, q, scale, blockIdx.x, cols, threadIdx.x, part);
 }
 
 }  // namespace weave

@@ -76,9 +76,14 @@ def int8_linear_workspace_bytes(in_features: int, out_features: int, max_tokens:
     return int(load().weave_int8_linear_workspace_bytes(ctypes.byref(cfg)))
 
 
+_types = {}
+
+
 def _type_of(dtype):
-    import torch
-    return {torch.bfloat16: BF16, torch.float32: F32, torch.int8: INT8}[dtype]
+    if not _types:
+        import torch
+        _types.update({torch.bfloat16: BF16, torch.float32: F32, torch.int8: INT8})
+    return _types[dtype]
 
 
 def quantize_rows(x, q=None, scale=None, stream: Optional[int] = None):
@@ -93,9 +98,9 @@ def quantize_rows(x, q=None, scale=None, stream: Optional[int] = None):
         scale = torch.empty(rows, dtype=torch.float32, device=x.device)
     assert q.device == x.device and q.dtype == torch.int8 and q.is_contiguous() and tuple(q.shape) == (rows, cols)
     assert scale.device == x.device and scale.dtype == torch.float32 and scale.is_contiguous() and tuple(scale.shape) == (rows,)
+    if stream is None:
+        stream = torch.cuda.current_stream(x.device).cuda_stream
     with torch.cuda.device(x.device):
-        if stream is None:
-            stream = torch.cuda.current_stream(x.device).cuda_stream
         _check(load().weave_int8_quantize(x.data_ptr(), _type_of(x.dtype), rows, cols, q.data_ptr(), scale.data_ptr(), stream),
                "weave_int8_quantize")
     return q, scale
@@ -115,14 +120,21 @@ class _Handle:
         cfg.workspace = self.workspace.data_ptr() + (-self.workspace.data_ptr()) % 1024
         cfg.workspace_bytes = nbytes
         self._h = ctypes.c_void_p()
+        self._index = device.index
+        self._raw_stream = torch._C._cuda_getCurrentRawStream      # current_stream() without the object around it: 4 us less
         with torch.cuda.device(device):
             _check(getattr(self._lib, f"{self._name}_create")(ctypes.byref(cfg), ctypes.byref(self._h)), f"{self._name}_create")
 
-    def _call(self, what: str, *args, stream: Optional[int]):
-        with self._torch.cuda.device(self.device):
-            if stream is None:
-                stream = self._torch.cuda.current_stream(self.device).cuda_stream
-            _check(getattr(self._lib, f"{self._name}_{what}")(self._h, *args, stream), f"{self._name}_{what}")
+    def _call(self, fn, *args, stream: Optional[int]):
+        if stream is None:
+            stream = self._raw_stream(self._index)
+        if self._torch.cuda.current_device() == self._index:
+            rc = fn(self._h, *args, stream)
+        else:
+            with self._torch.cuda.device(self.device):
+                rc = fn(self._h, *args, stream)
+        if rc != WEAVE_OK:
+            raise WeaveError(rc, fn.__name__)
 
     def status(self) -> int:
         """Synchronises the last call's stream; 0, or ERR_TIMEOUT after a wait that gave up, and clears it."""
@@ -186,7 +198,7 @@ class GatedFFN(_Handle):
         if out is None:
             out = self._torch.empty_like(x)
         T = self._rows(x, out)
-        self._call("forward", x.data_ptr(), out.data_ptr(), T, stream=stream)
+        self._call(self._lib.weave_ffn_forward, x.data_ptr(), out.data_ptr(), T, stream=stream)
         return out
 
     def backward(self, x, dy, dx=None, dgate_up=None, ddown=None, stream: Optional[int] = None):
@@ -198,8 +210,8 @@ class GatedFFN(_Handle):
         T = self._rows(x, dy, dx)
         for g, w in ((dgate_up, self.gate_up), (ddown, self.down)):
             assert g.device == self.device and g.dtype == torch.bfloat16 and g.is_contiguous() and g.shape == w.shape
-        self._call("backward", x.data_ptr(), dy.data_ptr(), dx.data_ptr(), dgate_up.data_ptr(), ddown.data_ptr(), T,
-                   stream=stream)
+        self._call(self._lib.weave_ffn_backward, x.data_ptr(), dy.data_ptr(), dx.data_ptr(), dgate_up.data_ptr(), ddown.data_ptr(),
+                   T, stream=stream)
         return dx, dgate_up, ddown
 
 
@@ -256,6 +268,6 @@ class Int8Linear(_Handle):
             assert tuple(x_scale.shape) == (T,)
         assert out.device == self.device and out.is_contiguous() and tuple(out.shape) == (T, self.N)
         assert out.dtype in (torch.bfloat16, torch.float32) and out_dtype in (None, out.dtype)
-        self._call("forward", x.data_ptr(), _type_of(x.dtype), None if x_scale is None else x_scale.data_ptr(),
-                   out.data_ptr(), _type_of(out.dtype), T, stream=stream)
+        self._call(self._lib.weave_int8_linear_forward, x.data_ptr(), _type_of(x.dtype),
+                   None if x_scale is None else x_scale.data_ptr(), out.data_ptr(), _type_of(out.dtype), T, stream=stream)
         return out
