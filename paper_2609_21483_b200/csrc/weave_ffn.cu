@@ -222,20 +222,13 @@ cudaError_t launch_small(const Engine &e, SmallArgs &a, int T, cudaStream_t stre
     a.ctl = e.ctl;
     a.timeout_ns = e.timeout_ns;
     a.T = T;
-    int w = 0, x = 0, cols = 16;
+    a.acc_cols = 0;
     for (int i = 0; i < a.products; ++i) {
-        const SmallShape &s = a.p[i].s;
-        w = s.w_bytes > w ? s.w_bytes : w;
-        x = s.x_bytes > x ? s.x_bytes : x;
-        cols = s.kbs * s.box_t > cols ? s.kbs * s.box_t : cols;
+        const int cols = a.p[i].s.kbs * a.p[i].s.box_t;
+        a.acc_cols = cols > a.acc_cols ? cols : a.acc_cols;
     }
-    a.x_offset = (int)up1024(w);
-    a.slot_bytes = a.x_offset + (int)up1024(x);
-    a.slots = kSmallMaxSlots;
-    while (small_smem_bytes(a.slots, a.slot_bytes) > kSmallSmemMax) --a.slots;
-    a.acc_cols = cols;
-    for (a.tmem_cols = 32; a.tmem_cols < 2 * cols;) a.tmem_cols *= 2;
-    return launch(weave_ffn_small_kernel<kI8>, e.n_sm, kSmallThreads, small_smem_bytes(a.slots, a.slot_bytes), kCooperative, stream, a);
+    for (a.tmem_cols = 32; a.tmem_cols < 2 * a.acc_cols;) a.tmem_cols *= 2;
+    return launch(weave_ffn_small_kernel<kI8>, e.n_sm, kSmallThreads, kSmallSmemMax, kCooperative, stream, a);
 }
 
 template <int kEpi, bool kI8, bool kAMn, bool kBMn>

@@ -104,11 +104,9 @@ __device__ __forceinline__ bool named_barrier_and(bool mine)
         : "memory");
     return all != 0;
 }
-__device__ __forceinline__ unsigned long long atom_acqrel_add_u64(unsigned long long *p, unsigned long long v)
+__device__ __forceinline__ void red_release_add_u64(unsigned long long *p, unsigned long long v)
 {
-    unsigned long long old;
-    asm volatile("atom.acq_rel.gpu.global.add.u64 %0, [%1], %2;" : "=l"(old) : "l"(p), "l"(v) : "memory");
-    return old;
+    asm volatile("red.release.gpu.global.add.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory");
 }
 __device__ __forceinline__ unsigned long long ld_acquire_u64(const unsigned long long *p)
 {
@@ -124,6 +122,8 @@ constexpr int kSmallMaxT = 128;
 constexpr int kSmallMaxSlots = 16;
 constexpr int kSmallRed = 128 * 9 * 4;           // an epilogue group's exchange buffer: 128 rows x 8 tokens, padded
 constexpr int kSmallSmemMax = 232448;
+constexpr int kSmallTail = 16384;                // behind the ring: exchange buffers and barriers
+constexpr int kSmallRing = kSmallSmemMax - 1024 - kSmallTail;
 
 // one product: how its columns are cut into tiles and its K into steps
 struct SmallShape {
@@ -135,12 +135,27 @@ struct SmallShape {
     int steps;           // steps of a tile
     int box_t;           // tokens of a block, padded
     int w_bytes, x_bytes;
+    int slots, slot_bytes, x_offset;     // of the ring while this product runs
 };
 
 __host__ __device__ inline int small_box(int T, int kbs)
 {
     const int b = T <= 8 ? 8 : T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128;
     return b == 8 && kbs == 1 ? 16 : b;          // N is a multiple of 16
+}
+
+// The ring's slots have another size in the second product.  Its first one is the first that starts behind the slot the
+// first product wrote last, so that slots are taken over in the order in which they become free.
+__device__ __forceinline__ int small_first_slot(const SmallShape &before, const SmallShape &s, int steps_before)
+{
+    const int at = (steps_before % before.slots * before.slot_bytes + s.slot_bytes - 1) / s.slot_bytes;
+    return at < s.slots ? at : 0;
+}
+// steps of a CTA's tiles
+__device__ __forceinline__ int small_steps(const SmallShape &s)
+{
+    const int tiles = (s.n + s.ct - 1) / s.ct, first = blockIdx.x * s.rounds;
+    return max(0, min(s.rounds, tiles - first)) * s.steps;
 }
 
 // block: elements of K in 128 bytes
@@ -164,6 +179,10 @@ inline SmallShape small_shape(int n, bool gated, long long K, int block, int T, 
     s.steps = (int)((blocks + s.kbs - 1) / s.kbs);
     s.w_bytes = s.kbs * s.rows * 128;
     s.x_bytes = s.kbs * s.box_t * 128;
+    s.x_offset = (s.w_bytes + 1023) & ~1023;
+    s.slot_bytes = s.x_offset + ((s.x_bytes + 1023) & ~1023);
+    s.slots = kSmallRing / s.slot_bytes;
+    if (s.slots > kSmallMaxSlots) s.slots = kSmallMaxSlots;
     return s;
 }
 
@@ -189,38 +208,39 @@ struct alignas(64) SmallArgs {
     FfnCtl *ctl;
     unsigned long long timeout_ns;
     int products, T;
-    int slots, slot_bytes, x_offset;
     int acc_cols, tmem_cols;
 };
 
 struct SmallBars {
-    uint64_t full[kSmallMaxSlots], empty[kSmallMaxSlots];
+    uint64_t full[2][kSmallMaxSlots], empty[2][kSmallMaxSlots];      // [product]
     uint64_t acc_full[2], acc_empty[2];
     uint64_t tokens[2];          // the tokens of product i are in memory
     uint32_t tmem_base;
     uint32_t row_max[8];
+    float row_scale[kSmallMaxT];
 };
-
-__host__ __device__ inline int small_smem_bytes(int slots, int slot_bytes)
-{
-    // a product reads 128 rows from the start of a slot, whatever it holds: 16 KB from the last slot's start on are ours
-    const int tail = 2 * kSmallRed + (int)sizeof(SmallBars);
-    const int reach = 16384 - slot_bytes;
-    return 1024 + slots * slot_bytes + (tail > reach ? tail : reach);
-}
+// a product reads 128 rows from the start of a slot, whatever it holds: the 16 KB behind the ring are ours, too
+static_assert(2 * kSmallRed + sizeof(SmallBars) <= kSmallTail, "the tail of shared memory");
 
 // All CTAs' epilogue warps arrive here with what they wrote; true when everybody has.  The counter only grows, by the
-// grid size per barrier and launch, so nothing has to be reset.
-__device__ __forceinline__ bool small_grid_barrier(unsigned long long *counter, bool ok, const WaitCtx &wc, int where)
+// grid size per barrier and launch, so nothing has to be reset; what it will reach is known to whoever reads it before
+// his own arrival (small_barrier_target).
+__device__ __forceinline__ unsigned long long small_barrier_target(const unsigned long long *counter)
+{
+    const unsigned long long g = gridDim.x;
+    return (ld_acquire_u64(counter) / g + 1) * g;
+}
+__device__ __forceinline__ bool small_grid_barrier(unsigned long long *counter, unsigned long long target, bool ok, const WaitCtx &wc, int where)
 {
     __threadfence();
     fence_proxy_async_global();          // ordinary stores here, tensor-map loads there
     ok = named_barrier_and<1, 256>(ok);
     if (ok && threadIdx.x == 128) {
-        const unsigned long long g = gridDim.x, old = atom_acqrel_add_u64(counter, 1ull), target = (old / g + 1) * g;
+        red_release_add_u64(counter, 1ull);
         unsigned long long t0 = 0;
         unsigned it = 0;
         while (ld_acquire_u64(counter) < target) {
+            __nanosleep(64);             // 148 of these loads at once would keep the last arrivals from the counter
             if ((++it & 31u) == 0u) {
                 if (*reinterpret_cast<volatile int *>(&wc.ctl->status) != 0) { ok = false; break; }
                 const unsigned long long now = globaltimer_ns();
@@ -250,14 +270,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
 {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    uint8_t *const behind = smem_raw + (smem - smem_u32(smem_raw)) + a.slots * a.slot_bytes;
+    uint8_t *const behind = smem_raw + (smem - smem_u32(smem_raw)) + kSmallRing;
     SmallBars &bars = *reinterpret_cast<SmallBars *>(behind + 2 * kSmallRed);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const WaitCtx wc = {a.ctl, a.timeout_ns};
     constexpr int kBlock = kI8 ? 128 : 64;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < a.slots; ++i) { mbar_init(&bars.full[i], 2); mbar_init(&bars.empty[i], 1); }
+        for (int i = 0; i < kSmallMaxSlots; ++i)
+            for (int j = 0; j < 2; ++j) { mbar_init(&bars.full[j][i], 2); mbar_init(&bars.empty[j][i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&bars.acc_full[i], 1); mbar_init(&bars.acc_empty[i], 8); mbar_init(&bars.tokens[i], 1); }
         fence_mbar_init();
     }
@@ -272,10 +293,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
         // ---- producers: warp 0 the weights, warp 1 the tokens
         if (lane == 0) {
             const bool weights = warp == 0;
-            int slot = 0;
-            uint32_t ph = 0;
-            for (int i = 0; i < a.products && ok; ++i) {
+#pragma unroll          // both products' parameters at fixed places of the constant bank
+            for (int i = 0; i < 2; ++i) {
+                if (i >= a.products || !ok) break;
                 const SmallProduct &p = a.p[i];
+                const int before = i > 0 ? small_steps(a.p[0].s) : 0, start = i > 0 ? small_first_slot(a.p[0].s, p.s, before) : 0;
+                const int turns = i > 0 ? before / a.p[0].s.slots : 0, rest = i > 0 ? before % a.p[0].s.slots : 0;
+                int slot = start, n = 0;
+                uint32_t ph = 0;
                 tma_prefetch_desc(weights ? &p.w : &p.x);
                 if (!weights && (i > 0 || (kI8 && p.round_src))) {
                     ok = ffn_wait(&bars.tokens[i], 0, wc, 20 + i);
@@ -286,14 +311,26 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
                     const int col0 = (blockIdx.x * p.s.rounds + r) * p.s.ct;
                     if (col0 >= p.s.n) break;
                     for (int k = 0; k < p.s.steps; ++k) {
-                        ok = ffn_wait(&bars.empty[slot], ph ^ 1u, wc, 22 + (int)weights);
+                        if (i == 0 || n >= p.s.slots) {
+                            ok = ffn_wait(&bars.empty[i][slot], ph ^ 1u, wc, 22 + (int)weights);
+                        } else if (weights) {
+                            // first use of a slot: the newest step of the product before that lies in it.  (Tokens come
+                            // behind the grid barrier, when all of those are done with.)
+                            const SmallShape &o = a.p[0].s;
+                            int j = min(o.slots - 1, ((slot + 1) * p.s.slot_bytes - 1) / o.slot_bytes);
+                            if (j >= rest && slot * p.s.slot_bytes < rest * o.slot_bytes) j = rest - 1;
+                            const int uses = turns + (j < rest ? 1 : 0);
+                            if (uses > 0) ok = ffn_wait(&bars.empty[0][j], (uint32_t)(uses - 1) & 1u, wc, 23);
+                        }
                         if (!ok) break;
-                        uint64_t *full = &bars.full[slot];
-                        const uint32_t dst = smem + slot * a.slot_bytes;
+                        uint64_t *full = &bars.full[i][slot];
+                        const uint32_t dst = smem + slot * p.s.slot_bytes;
                         mbar_arrive_expect_tx(full, (uint32_t)(weights ? p.s.w_bytes : p.s.x_bytes));
                         if (weights) tma_load_4d_one(dst, &p.w, one ? k * kBlock : 0, col0, 0, one ? 0 : k * p.s.kbs, full);
-                        else tma_load_3d_one(dst + a.x_offset, &p.x, one ? k * kBlock : 0, 0, one ? 0 : k * p.s.kbs, full);
-                        if (++slot == a.slots) { slot = 0; ph ^= 1u; }
+                        else tma_load_3d_one(dst + p.s.x_offset, &p.x, one ? k * kBlock : 0, 0, one ? 0 : k * p.s.kbs, full);
+                        ++n;
+                        if (++slot == p.s.slots) slot = 0;
+                        if (slot == start) ph ^= 1u;
                     }
                 }
             }
@@ -302,10 +339,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
         __syncwarp();
     } else if (warp == 2) {
         if (lane == 0) {
-            int slot = 0, n = 0;
-            uint32_t ph = 0;
-            for (int i = 0; i < a.products && ok; ++i) {
+            int n = 0;
+#pragma unroll          // both products' parameters at fixed places of the constant bank
+            for (int i = 0; i < 2; ++i) {
+                if (i >= a.products || !ok) break;
                 const SmallShape &s = a.p[i].s;
+                const int start = i > 0 ? small_first_slot(a.p[0].s, s, small_steps(a.p[0].s)) : 0;
+                int slot = start;
+                uint32_t ph = 0;
                 const uint32_t idesc = kI8 ? umma_idesc_i8(128, s.kbs * s.box_t) : umma_idesc_bf16(128, s.kbs * s.box_t);
                 for (int r = 0; r < s.rounds && ok; ++r, ++n) {
                     if ((blockIdx.x * s.rounds + r) * s.ct >= s.n) break;
@@ -313,14 +354,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
                     ok = ffn_wait(&bars.acc_empty[buf], ((n >> 1) & 1) ^ 1, wc, 24);
                     tc_fence_after();
                     for (int k = 0; k < s.steps && ok; ++k) {
-                        ok = ffn_wait(&bars.full[slot], ph, wc, 25);
+                        ok = ffn_wait(&bars.full[i][slot], ph, wc, 25);
                         if (!ok) break;
                         tc_fence_after();
-                        const uint32_t w = smem + slot * a.slot_bytes;
-                        ffn_mma_kstep_one<kI8>(tmem + (uint32_t)(buf * a.acc_cols), umma_desc_sw128(w), umma_desc_sw128(w + a.x_offset), idesc,
+                        const uint32_t w = smem + slot * s.slot_bytes;
+                        ffn_mma_kstep_one<kI8>(tmem + (uint32_t)(buf * a.acc_cols), umma_desc_sw128(w), umma_desc_sw128(w + s.x_offset), idesc,
                                                (uint32_t)(k != 0));
-                        tc_commit_one(&bars.empty[slot]);
-                        if (++slot == a.slots) { slot = 0; ph ^= 1u; }
+                        tc_commit_one(&bars.empty[i][slot]);
+                        if (++slot == s.slots) slot = 0;
+                        if (slot == start) ph ^= 1u;
                     }
                     if (ok) tc_commit_one(&bars.acc_full[buf]);
                 }
@@ -333,13 +375,18 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
         // lanes of its number mod 4
         const int quarter = warp & 3, group = (warp - 4) >> 2, tid = threadIdx.x - 128 - group * 128;
         const int acc_row = quarter * 32 + lane;
-        float *const red_f = reinterpret_cast<float *>(behind + group * kSmallRed);
-        uint32_t *const red = reinterpret_cast<uint32_t *>(red_f);
-        int n = 0, barrier = 0;
-        for (int i = 0; i < a.products && ok; ++i) {
+        uint32_t *const red = reinterpret_cast<uint32_t *>(behind + group * kSmallRed);
+        unsigned long long target[3] = {0, 0, 0};
+        if (threadIdx.x == 128)
+#pragma unroll
+            for (int j = 0; j < 3; ++j) target[j] = small_barrier_target(&a.ctl->barrier[j]);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (i >= a.products || !ok) break;
             const SmallProduct &p = a.p[i];
             const SmallShape &s = p.s;
-            if (i > 0) ok = small_grid_barrier(&a.ctl->barrier[barrier++], ok, wc, 26);
+            if (i > 0) ok = small_grid_barrier(&a.ctl->barrier[0], target[0], ok, wc, 26);
             if constexpr (kI8) {
                 if (ok && p.round_src) {
                     for (int row = blockIdx.x; row < a.T; row += gridDim.x) {
@@ -352,59 +399,79 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
                                                                          row, p.K, tid256, bars.row_max);
                         named_barrier_sync<1, 256>();
                     }
-                    ok = small_grid_barrier(&a.ctl->barrier[barrier++], ok, wc, 27);
+                    ok = small_grid_barrier(&a.ctl->barrier[1 + i], i == 0 ? target[1] : target[2], ok, wc, 27);
                 }
             }
             if (!ok) break;
             if (threadIdx.x == 128) mbar_arrive(&bars.tokens[i]);
+            if constexpr (kI8) {
+                // (read behind the barriers in the tile's loop)
+                for (int t = threadIdx.x - 128; t < a.T; t += 256) bars.row_scale[t] = __ldcg(p.row_scale + t);
+            }
             const int blocks_from = quarter * 32 / s.rows, blocks_to = min(s.kbs - 1, (quarter * 32 + 31) / s.rows), mine = acc_row / s.rows;
+            int pow2 = 1;
+            while (pow2 < s.ct) pow2 *= 2;
             for (int r = 0; r < s.rounds; ++r, ++n) {
                 const int col0 = (blockIdx.x * s.rounds + r) * s.ct;
                 if (col0 >= s.n) break;
                 const int cols = min(s.ct, s.n - col0), buf = n & 1;
+                // a thread's column of the tile, and which of the eight tokens it starts with
+                const int c = tid & (pow2 - 1), t_first = tid / pow2, t_step = 128 / pow2;
+                float sw0 = 0.0f, sw1 = 0.0f;
+                if constexpr (kI8) {
+                    if (c < cols) {
+                        sw0 = p.col_scale[col0 + c];
+                        if (p.gated) sw1 = p.col_scale[s.n + col0 + c];
+                    }
+                }
                 ok = ffn_wait(&bars.acc_full[buf], (n >> 1) & 1, wc, 28);
                 ok = named_barrier_and<1, 256>(ok);       // barriers follow: all warps leave together
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t acc = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * a.acc_cols);
                 for (int t0 = group * 8; t0 < a.T; t0 += 16) {
+                    uint32_t v[8];
                     for (int b = blocks_from; b <= blocks_to; ++b) {
-                        uint32_t v[8];
-                        tmem_ld_32x8(acc + (uint32_t)(b * s.box_t + t0), v);
-                        tmem_ld_wait8(v);
-                        if (b == mine) {
+                        uint32_t w[8];
+                        tmem_ld_32x8(acc + (uint32_t)(b * s.box_t + t0), w);
+                        tmem_ld_wait8(w);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) red[acc_row * 9 + j] = v[j];
-                        }
-                        __syncwarp();
+                        for (int j = 0; j < 8; ++j) v[j] = b == mine || b == blocks_from ? w[j] : v[j];
+                    }
+                    if (blocks_from <= blocks_to) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) red[acc_row * 9 + j] = v[j];
                     }
                     if (group == 0) named_barrier_sync<2, 128>();
                     else named_barrier_sync<3, 128>();
                     const int left = min(8, a.T - t0);
-                    for (int at = tid; at < cols * left; at += 128) {
-                        const int t = at / cols, c = at - t * cols;
-                        uint32_t sum0 = red[c * 9 + t], sum1 = p.gated ? red[(s.ct + c) * 9 + t] : 0u;
-                        for (int b = 1; b < s.kbs; ++b) {
-                            const int o = (b * s.rows + c) * 9 + t;
-                            if constexpr (kI8) {
-                                sum0 += red[o];
-                                if (p.gated) sum1 += red[o + s.ct * 9];
-                            } else {
-                                sum0 = __float_as_uint(__uint_as_float(sum0) + red_f[o]);
-                                if (p.gated) sum1 = __float_as_uint(__uint_as_float(sum1) + red_f[o + s.ct * 9]);
+                    if (c < cols) {
+                        uint8_t *const to = static_cast<uint8_t *>(p.out) + ((long long)(t0 + t_first) * s.n + col0 + c) * (p.out_f32 ? 4 : 2);
+                        const int step_bytes = s.n * t_step * (p.out_f32 ? 4 : 2);
+                        const uint32_t *const from = red + c * 9 + t_first;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int t = t_first + j * t_step;
+                            if (t >= left) break;
+                            const uint32_t *const v = from + j * t_step;
+                            uint32_t sum0 = v[0], sum1 = p.gated ? v[s.ct * 9] : 0u;
+                            for (int b = 1; b < s.kbs; ++b) {
+                                const uint32_t *const w = v + b * s.rows * 9;
+                                if constexpr (kI8) {
+                                    sum0 += w[0];
+                                    if (p.gated) sum1 += w[s.ct * 9];
+                                } else {
+                                    sum0 = __float_as_uint(__uint_as_float(sum0) + __uint_as_float(w[0]));
+                                    if (p.gated) sum1 = __float_as_uint(__uint_as_float(sum1) + __uint_as_float(w[s.ct * 9]));
+                                }
                             }
+                            const float sx = kI8 ? bars.row_scale[t0 + t] : 0.0f;
+                            float y = small_value<kI8>(sum0, sx, sw0);
+                            if (p.gated) y = gated(y, small_value<kI8>(sum1, sx, sw1));
+                            uint8_t *const at = to + (long long)j * step_bytes;
+                            if (p.out_f32) *reinterpret_cast<float *>(at) = y;
+                            else *reinterpret_cast<__nv_bfloat16 *>(at) = __float2bfloat16_rn(y);
                         }
-                        float sx = 0.0f, sw0 = 0.0f, sw1 = 0.0f;
-                        if constexpr (kI8) {
-                            sx = __ldcg(p.row_scale + t0 + t);
-                            sw0 = p.col_scale[col0 + c];
-                            if (p.gated) sw1 = p.col_scale[s.n + col0 + c];
-                        }
-                        float y = small_value<kI8>(sum0, sx, sw0);
-                        if (p.gated) y = gated(y, small_value<kI8>(sum1, sx, sw1));
-                        const long long where = (long long)(t0 + t) * s.n + col0 + c;
-                        if (p.out_f32) static_cast<float *>(p.out)[where] = y;
-                        else static_cast<__nv_bfloat16 *>(p.out)[where] = __float2bfloat16_rn(y);
                     }
                     if (group == 0) named_barrier_sync<2, 128>();
                     else named_barrier_sync<3, 128>();
