@@ -21,6 +21,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
 
 constexpr int kMaxWidth = 65536;
 constexpr int kMaxRows = 1 << 22;
+constexpr int kMaxSms = 160;
 
 size_t up1024(size_t n) { return (n + 1023) & ~(size_t)1023; }
 
@@ -82,7 +83,7 @@ int engine_create(Engine &e, void *workspace)
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, e.device) != cudaSuccess)
         return WEAVE_ERR_CUDA;
     if (major != 10 || smem < kSmallSmemMax || sms < 2) return WEAVE_ERR_UNSUPPORTED_DEVICE;
-    e.n_sm = sms & ~1;
+    e.n_sm = (sms < kMaxSms ? sms : kMaxSms) & ~1;
     e.ctl = static_cast<FfnCtl *>(workspace);
     e.timeout_ns = 4000ull * 1000000ull;
     e.last_stream = nullptr;
@@ -178,34 +179,52 @@ cudaError_t launch(void (*kernel)(Params...), int grid, int block, size_t smem, 
     return cudaLaunchKernelEx(&lc, kernel, args...);
 }
 
-// The first product of a, or the next one: its plan and its tensor maps.  x: what the product reads, [T][K].
+// The first product of a, or the next one: its plan and its tensor maps.  x: what the product reads, [copies][T][K].
 bool small_product(const Engine &e, SmallArgs &a, int type, const void *w, const void *x, int n, bool gated, int K, int T, const float *row_scale,
-                   const float *col_scale, void *out, bool out_f32)
+                   const float *col_scale, void *out, bool out_f32, int copies)
 {
     SmallProduct &p = a.p[a.products++];
     const int size = type == WEAVE_INT8 ? 1 : 2, block = 128 / size;
-    p.s = small_shape(n, gated, K, block, T, e.n_sm);
+    p.s = small_plan(n, gated, K, block, T, e.n_sm);
     p.gated = gated;
     p.out_f32 = out_f32;
     p.row_scale = row_scale;
     p.col_scale = col_scale;
     p.out = out;
     p.round_src = nullptr;
+    p.round_local = copies > 1;
     p.K = K;
     // with several blocks of K per step they are the maps' last dimension; with one, K is the first, clipped at its end
     const bool blocks = p.s.kbs > 1;
     const cuuint64_t row = (cuuint64_t)K * size, inner = blocks ? (cuuint64_t)block : (cuuint64_t)K, count = blocks ? (cuuint64_t)(K / block) : 1;
     const cuuint64_t wd[4] = {inner, (cuuint64_t)n, gated ? 2u : 1u, count}, ws[3] = {row, row * (cuuint64_t)n, 128};
     const cuuint32_t wb[4] = {(cuuint32_t)block, (cuuint32_t)p.s.ct, gated ? 2u : 1u, (cuuint32_t)p.s.kbs};
-    const cuuint64_t xd[3] = {inner, (cuuint64_t)T, count}, xs[2] = {row, 128};
-    const cuuint32_t xb[3] = {(cuuint32_t)block, (cuuint32_t)p.s.box_t, (cuuint32_t)p.s.kbs};
+    const cuuint64_t xd[4] = {inner, (cuuint64_t)T, count, (cuuint64_t)copies}, xs[3] = {row, 128, row * (cuuint64_t)T};
+    const cuuint32_t xb[4] = {(cuuint32_t)block, (cuuint32_t)p.s.box_t, (cuuint32_t)p.s.kbs, 1};
     const cuuint32_t ones[4] = {1, 1, 1, 1};
     const CUtensorMapDataType dt = size == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     return e.encode(&p.w, dt, 4, const_cast<void *>(w), wd, ws, wb, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS &&
-           e.encode(&p.x, dt, 3, const_cast<void *>(x), xd, xs, xb, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           e.encode(&p.x, dt, 4, const_cast<void *>(x), xd, xs, xb, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+// Up to two tokens every CTA rounds for itself, 1.4 us each; from three on one row per CTA and a grid barrier behind them
+// (3 to 4 us while the ring fills) take less.
+constexpr int kSmallLocalT = 2, kSmallLocalK = 16384;
+int small_copies(const Engine &e, int T, int K) { return T <= kSmallLocalT && K <= kSmallLocalK ? e.n_sm : 1; }
+// scratch for the integers of a first product's tokens, and for their scales
+size_t small_round_bytes(int max_tokens, int K)
+{
+    const size_t all = (size_t)max_tokens * K;
+    const size_t copies = K <= kSmallLocalK ? (size_t)kMaxSms * (max_tokens < kSmallLocalT ? max_tokens : kSmallLocalT) * K : 0;
+    return all > copies ? all : copies;
+}
+size_t small_round_scales(int max_tokens)
+{
+    const size_t copies = (size_t)kMaxSms * kSmallLocalT;
+    return ((size_t)max_tokens > copies ? (size_t)max_tokens : copies) * 4;
+}
+
 // tokens that the kernel rounds to integers before the product made last
 void small_round(SmallArgs &a, const void *src, int src_type, int8_t *dst, float *scale)
 {
@@ -292,7 +311,7 @@ FfnLayout ffn_layout(const weave_ffn_config *c)
 {
     FfnLayout L;
     memset(&L, 0, sizeof(L));
-    const size_t T = (size_t)c->max_tokens, H = (size_t)c->hidden, I = (size_t)c->ffn;
+    const size_t T = (size_t)c->max_tokens, I = (size_t)c->ffn;
     size_t at = up1024(sizeof(FfnCtl));
     L.control = at;
     L.h = at;
@@ -303,9 +322,9 @@ FfnLayout ffn_layout(const weave_ffn_config *c)
     }
     if (c->weight_type == WEAVE_INT8) {
         L.xq = at;
-        at += up1024(T * H);
+        at += up1024(small_round_bytes(c->max_tokens, c->hidden));
         L.x_scale = at;
-        at += up1024(T * 4);
+        at += up1024(small_round_scales(c->max_tokens));
         L.hq = at;
         at += up1024(T * I);
         L.h_scale = at;
@@ -387,9 +406,11 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     if (T <= kSmallMaxT) {
         SmallArgs a;
         a.products = 0;
-        if (!small_product(h->e, a, type, h->cfg.gate_up, left, I, true, H, T, xs, h->cfg.gate_up_scale, hbuf, false)) return WEAVE_ERR_CUDA;
+        if (!small_product(h->e, a, type, h->cfg.gate_up, left, I, true, H, T, xs, h->cfg.gate_up_scale, hbuf, false,
+                           i8 ? small_copies(h->e, T, H) : 1))
+            return WEAVE_ERR_CUDA;
         if (i8) small_round(a, x, WEAVE_BF16, xq, xs);
-        if (!small_product(h->e, a, type, h->cfg.down, mid, H, false, I, T, hs, h->cfg.down_scale, out, false)) return WEAVE_ERR_CUDA;
+        if (!small_product(h->e, a, type, h->cfg.down, mid, H, false, I, T, hs, h->cfg.down_scale, out, false, 1)) return WEAVE_ERR_CUDA;
         if (i8) small_round(a, hbuf, WEAVE_BF16, hq, hs);
         err = i8 ? launch_small<true>(h->e, a, T, stream) : launch_small<false>(h->e, a, T, stream);
         return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
@@ -508,9 +529,9 @@ Int8Layout int8_layout(const weave_int8_linear_config *c)
     size_t at = up1024(sizeof(FfnCtl));
     L.control = at;
     L.xq = at;
-    at += up1024((size_t)c->max_tokens * c->in_features);
+    at += up1024(small_round_bytes(c->max_tokens, c->in_features));
     L.x_scale = at;
-    at += up1024((size_t)c->max_tokens * 4);
+    at += up1024(small_round_scales(c->max_tokens));
     L.total = at;
     return L;
 }
@@ -594,7 +615,8 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     if (T <= kSmallMaxT) {
         SmallArgs a;
         a.products = 0;
-        if (!small_product(h->e, a, WEAVE_INT8, h->cfg.weight, q, N, false, K, T, x_scale, h->cfg.scale, out, out_type == WEAVE_F32))
+        if (!small_product(h->e, a, WEAVE_INT8, h->cfg.weight, q, N, false, K, T, x_scale, h->cfg.scale, out, out_type == WEAVE_F32,
+                           round ? small_copies(h->e, T, K) : 1))
             return WEAVE_ERR_CUDA;
         if (round) small_round(a, x, x_type, xq, xs);
         err = launch_small<true>(h->e, a, T, stream);

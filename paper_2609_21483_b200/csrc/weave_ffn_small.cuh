@@ -38,42 +38,51 @@ __device__ __forceinline__ void tmem_dealloc_one(uint32_t taddr, uint32_t ncols)
 {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
 }
-__device__ __forceinline__ void tc_commit_one(uint64_t *bar)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// four products over 128 bytes of K, K-major operands; called by one thread
+// The forms below are called by a whole converged warp; the elected thread issues, everything else stays
+// warp-uniform, so that operands live in uniform registers (from one lane of a divergent branch a step of the ring took
+// 330 ns however little it moved).
+
+// four products over 128 bytes of K, K-major operands, and the commit that frees their slot
 template <bool kI8>
-__device__ __forceinline__ void ffn_mma_kstep_one(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate_first)
+__device__ __forceinline__ void ffn_mma_kstep_one(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate_first,
+                                                  uint64_t *empty_bar)
 {
 #define WEAVE_KSTEP_ONE(KIND)                                                                   \
     asm volatile(                                                                               \
-        "{\n\t.reg .pred pa, pt;\n\t"                                                           \
+        "{\n\t.reg .pred pe, pa, pt;\n\t"                                                       \
         ".reg .b64 a1, a2, a3, b1, b2, b3;\n\t"                                                 \
+        "elect.sync _|pe, 0xffffffff;\n\t"                                                      \
         "setp.ne.b32 pa, %4, 0;\n\t"                                                            \
         "setp.eq.u32 pt, %0, %0;\n\t"                                                           \
         "add.u64 a1, %1, 2;\n\tadd.u64 a2, %1, 4;\n\tadd.u64 a3, %1, 6;\n\t"                    \
         "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"                    \
-        "tcgen05.mma.cta_group::1.kind::" KIND " [%0], %1, %2, %3, pa;\n\t"                     \
-        "tcgen05.mma.cta_group::1.kind::" KIND " [%0], a1, b1, %3, pt;\n\t"                     \
-        "tcgen05.mma.cta_group::1.kind::" KIND " [%0], a2, b2, %3, pt;\n\t"                     \
-        "tcgen05.mma.cta_group::1.kind::" KIND " [%0], a3, b3, %3, pt;\n\t}"                    \
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate_first) : "memory")
+        "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], %1, %2, %3, pa;\n\t"                 \
+        "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], a1, b1, %3, pt;\n\t"                 \
+        "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], a2, b2, %3, pt;\n\t"                 \
+        "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], a3, b3, %3, pt;\n\t"                 \
+        "@pe tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t}"  \
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate_first), "r"(smem_u32(empty_bar)) : "memory")
     if (kI8) WEAVE_KSTEP_ONE("i8");
     else WEAVE_KSTEP_ONE("f16");
 #undef WEAVE_KSTEP_ONE
 }
-__device__ __forceinline__ void tma_load_3d_one(uint32_t dst, const void *map, int x, int y, int z, uint64_t *bar)
+__device__ __forceinline__ void tc_commit_one(uint64_t *bar)
 {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
-                 : "memory");
+    asm volatile(
+        "{\n\t.reg .pred pe;\n\t"
+        "elect.sync _|pe, 0xffffffff;\n\t"
+        "@pe tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void tma_load_4d_one(uint32_t dst, const void *map, int x, int y, int z, int w, uint64_t *bar)
+// arrival with the byte count, and the copy
+__device__ __forceinline__ void tma_fill(uint32_t dst, const void *map, int x, int y, int z, int w, uint64_t *bar, uint32_t bytes)
 {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
-                 : "memory");
+    asm volatile(
+        "{\n\t.reg .pred pe;\n\t"
+        "elect.sync _|pe, 0xffffffff;\n\t"
+        "@pe mbarrier.arrive.expect_tx.shared::cta.b64 _, [%6], %7;\n\t"
+        "@pe cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar)), "r"(bytes)
+        : "memory");
 }
 // 32 lanes x 8 consecutive columns
 __device__ __forceinline__ void tmem_ld_32x8(uint32_t taddr, uint32_t (&r)[8])
@@ -120,7 +129,8 @@ __device__ __forceinline__ unsigned long long ld_acquire_u64(const unsigned long
 constexpr int kSmallThreads = 384;               // weights, tokens, issuer, (idle), eight epilogue warps
 constexpr int kSmallMaxT = 128;
 constexpr int kSmallMaxSlots = 16;
-constexpr int kSmallRed = 128 * 9 * 4;           // an epilogue group's exchange buffer: 128 rows x 8 tokens, padded
+constexpr int kSmallRedRow = 12;                 // words of a row of an epilogue group's exchange buffer: 8 tokens, padded
+constexpr int kSmallRed = 128 * kSmallRedRow * 4;
 constexpr int kSmallSmemMax = 232448;
 constexpr int kSmallTail = 16384;                // behind the ring: exchange buffers and barriers
 constexpr int kSmallRing = kSmallSmemMax - 1024 - kSmallTail;
@@ -140,8 +150,7 @@ struct SmallShape {
 
 __host__ __device__ inline int small_box(int T, int kbs)
 {
-    const int b = T <= 8 ? 8 : T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128;
-    return b == 8 && kbs == 1 ? 16 : b;          // N is a multiple of 16
+    return kbs == 1 ? (T + 15) & ~15 : (T + 7) & ~7;          // N = kbs * box is a multiple of 16
 }
 
 // The ring's slots have another size in the second product.  Its first one is the first that starts behind the slot the
@@ -158,39 +167,56 @@ __device__ __forceinline__ int small_steps(const SmallShape &s)
     return max(0, min(s.rounds, tiles - first)) * s.steps;
 }
 
-// block: elements of K in 128 bytes
-inline SmallShape small_shape(int n, bool gated, long long K, int block, int T, int ctas)
+// The plan with kbs blocks of K per step; block: elements of K in 128 bytes.
+inline SmallShape small_shape(int n, bool gated, long long K, int block, int T, int ctas, int kbs)
 {
     SmallShape s;
     s.n = n;
-    const int most = gated ? 64 : 128;
+    const int most = 128 / (gated ? 2 * kbs : kbs);
     s.rounds = (int)((n + (long long)ctas * most - 1) / ((long long)ctas * most));
     s.ct = (int)((n + (long long)ctas * s.rounds - 1) / ((long long)ctas * s.rounds));
     s.rows = gated ? 2 * s.ct : s.ct;
+    s.kbs = kbs;
+    s.box_t = small_box(T, kbs);
     const long long blocks = (K + block - 1) / block;
-    s.kbs = 1;
-    if (K % block == 0)
-        // cycles per block of a product over kbs of them, half of N but at least 48; fewer only if that is worth it
-        for (int k = 2; k <= 8 && k * s.rows <= 128 && k * small_box(T, k) <= 256 && k <= blocks; k *= 2) {
-            const int now = small_box(T, s.kbs) * s.kbs / 2, then = small_box(T, k) * k / 2;
-            if ((then < 48 ? 48 : then) * s.kbs < (now < 48 ? 48 : now) * k) s.kbs = k;
-        }
-    s.box_t = small_box(T, s.kbs);
-    s.steps = (int)((blocks + s.kbs - 1) / s.kbs);
-    s.w_bytes = s.kbs * s.rows * 128;
-    s.x_bytes = s.kbs * s.box_t * 128;
+    s.steps = (int)((blocks + kbs - 1) / kbs);
+    s.w_bytes = kbs * s.rows * 128;
+    s.x_bytes = kbs * s.box_t * 128;
     s.x_offset = (s.w_bytes + 1023) & ~1023;
     s.slot_bytes = s.x_offset + ((s.x_bytes + 1023) & ~1023);
     s.slots = kSmallRing / s.slot_bytes;
     if (s.slots > kSmallMaxSlots) s.slots = kSmallMaxSlots;
     return s;
 }
+// Microseconds that a product takes with this plan, from measurements: the chip reads weights at 6.4 TB/s (a little less
+// where a step takes only 128 or 256 bytes of each row), an SM takes in 90 bytes per ns, weights and tokens, a step of the
+// ring is 250 ns at least, a tile's epilogue holds up the next one by some 0.15 us.  (16 tokens, 4096 -> 2 x 14336 -> 4096,
+// us for 1, 2, 4, 8 blocks per step in both products: 99, 72, 59.5, 63; 64 tokens with 1, 2, 4 in the first and 4 in the
+// second: 74, 78, 90; one token through 2048 x 768: 17.2, 12.6, 9.8, 9.6.)
+inline double small_cost(const SmallShape &s, long long K, int block, int T)
+{
+    const double weights = (double)s.n * (s.rows / s.ct) * ((double)K / block * 128.0);
+    const double chip = weights / (s.kbs == 1 ? 5900.0 : s.kbs == 2 ? 6100.0 : 6400.0);
+    const double steps = (double)s.rounds * s.steps;
+    const double sm = steps * (s.w_bytes + s.kbs * T * 128.0) / 90.0, issue = steps * 250.0;
+    return ((chip > sm ? chip : sm) > issue ? (chip > sm ? chip : sm) : issue) / 1000.0 + 0.15 * s.rounds;
+}
+inline SmallShape small_plan(int n, bool gated, long long K, int block, int T, int ctas)
+{
+    SmallShape best = small_shape(n, gated, K, block, T, ctas, 1);
+    if (K % block == 0)          // the maps of several blocks cannot clip the last one
+        for (int kbs = 2; kbs <= 8 && kbs <= K / block && kbs * small_box(T, kbs) <= 256; kbs *= 2) {
+            const SmallShape s = small_shape(n, gated, K, block, T, ctas, kbs);
+            if (small_cost(s, K, block, T) < small_cost(best, K, block, T)) best = s;
+        }
+    return best;
+}
 
 // ------------------------------------------------------------------------------------ the kernel
 
 struct alignas(64) SmallProduct {
     CUtensorMap w;           // {K, rows, halves, 1} or {block, rows, halves, blocks}
-    CUtensorMap x;           // {K, T, 1} or {block, T, blocks}
+    CUtensorMap x;           // {K, T, 1, copies} or {block, T, blocks, copies}
     SmallShape s;
     int gated, out_f32;
     const float *row_scale;  // 8-bit forms: [T], and [n] (gated: [2n], gate then up)
@@ -201,6 +227,7 @@ struct alignas(64) SmallProduct {
     int8_t *round_dst;
     float *round_scale;
     int round_f32, K;
+    int round_local;         // every CTA rounds all rows for itself, into a copy of its own
 };
 
 struct alignas(64) SmallArgs {
@@ -259,10 +286,31 @@ __device__ __forceinline__ bool small_grid_barrier(unsigned long long *counter, 
     return ok;
 }
 
+// The epilogue warps round the tokens of a product: one row per CTA, or all rows into this CTA's own copy.
+template <class X>
+__device__ __noinline__ void small_round_rows(const X *src, const SmallProduct &p, int T, uint32_t *part)
+{
+    const int tid = threadIdx.x - 128;
+    const size_t copy = p.round_local ? (size_t)blockIdx.x * T : 0;
+    for (int row = p.round_local ? 0 : blockIdx.x; row < T; row += p.round_local ? 1 : gridDim.x) {
+        quant_row_by<X, 256, 8, true, true>(src, p.round_dst + copy * p.K, p.round_scale + copy, row, p.K, tid, part);
+        named_barrier_sync<1, 256>();
+    }
+}
+
 template <bool kI8>
 __device__ __forceinline__ float small_value(uint32_t acc, float sx, float sw)
 {
     return kI8 ? __int2float_rn((int)acc) * (sx * sw) : __uint_as_float(acc);
+}
+
+template <bool kI8>
+__device__ __forceinline__ uint4 small_add(uint4 a, uint4 b)
+{
+    if constexpr (kI8) return make_uint4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+    else
+        return make_uint4(__float_as_uint(__uint_as_float(a.x) + __uint_as_float(b.x)), __float_as_uint(__uint_as_float(a.y) + __uint_as_float(b.y)),
+                          __float_as_uint(__uint_as_float(a.z) + __uint_as_float(b.z)), __float_as_uint(__uint_as_float(a.w) + __uint_as_float(b.w)));
 }
 
 template <bool kI8>
@@ -291,85 +339,80 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
     bool ok = true;
     if (warp < 2) {
         // ---- producers: warp 0 the weights, warp 1 the tokens
-        if (lane == 0) {
-            const bool weights = warp == 0;
+        const bool weights = warp == 0;
 #pragma unroll          // both products' parameters at fixed places of the constant bank
-            for (int i = 0; i < 2; ++i) {
-                if (i >= a.products || !ok) break;
-                const SmallProduct &p = a.p[i];
-                const int before = i > 0 ? small_steps(a.p[0].s) : 0, start = i > 0 ? small_first_slot(a.p[0].s, p.s, before) : 0;
-                const int turns = i > 0 ? before / a.p[0].s.slots : 0, rest = i > 0 ? before % a.p[0].s.slots : 0;
-                int slot = start, n = 0;
-                uint32_t ph = 0;
-                tma_prefetch_desc(weights ? &p.w : &p.x);
-                if (!weights && (i > 0 || (kI8 && p.round_src))) {
-                    ok = ffn_wait(&bars.tokens[i], 0, wc, 20 + i);
-                    fence_proxy_async_global();
-                }
-                const bool one = p.s.kbs == 1;
-                for (int r = 0; r < p.s.rounds && ok; ++r) {
-                    const int col0 = (blockIdx.x * p.s.rounds + r) * p.s.ct;
-                    if (col0 >= p.s.n) break;
-                    for (int k = 0; k < p.s.steps; ++k) {
-                        if (i == 0 || n >= p.s.slots) {
-                            ok = ffn_wait(&bars.empty[i][slot], ph ^ 1u, wc, 22 + (int)weights);
-                        } else if (weights) {
-                            // first use of a slot: the newest step of the product before that lies in it.  (Tokens come
-                            // behind the grid barrier, when all of those are done with.)
-                            const SmallShape &o = a.p[0].s;
-                            int j = min(o.slots - 1, ((slot + 1) * p.s.slot_bytes - 1) / o.slot_bytes);
-                            if (j >= rest && slot * p.s.slot_bytes < rest * o.slot_bytes) j = rest - 1;
-                            const int uses = turns + (j < rest ? 1 : 0);
-                            if (uses > 0) ok = ffn_wait(&bars.empty[0][j], (uint32_t)(uses - 1) & 1u, wc, 23);
-                        }
-                        if (!ok) break;
-                        uint64_t *full = &bars.full[i][slot];
-                        const uint32_t dst = smem + slot * p.s.slot_bytes;
-                        mbar_arrive_expect_tx(full, (uint32_t)(weights ? p.s.w_bytes : p.s.x_bytes));
-                        if (weights) tma_load_4d_one(dst, &p.w, one ? k * kBlock : 0, col0, 0, one ? 0 : k * p.s.kbs, full);
-                        else tma_load_3d_one(dst + p.s.x_offset, &p.x, one ? k * kBlock : 0, 0, one ? 0 : k * p.s.kbs, full);
-                        ++n;
-                        if (++slot == p.s.slots) slot = 0;
-                        if (slot == start) ph ^= 1u;
+        for (int i = 0; i < 2; ++i) {
+            if (i >= a.products || !ok) break;
+            const SmallProduct &p = a.p[i];
+            const int before = i > 0 ? small_steps(a.p[0].s) : 0, start = i > 0 ? small_first_slot(a.p[0].s, p.s, before) : 0;
+            const int turns = i > 0 ? before / a.p[0].s.slots : 0, rest = i > 0 ? before % a.p[0].s.slots : 0;
+            int slot = start, n = 0;
+            uint32_t ph = 0;
+            if (lane == 0) tma_prefetch_desc(weights ? &p.w : &p.x);
+            if (!weights && (i > 0 || (kI8 && p.round_src))) {
+                ok = __all_sync(0xffffffffu, ffn_wait(&bars.tokens[i], 0, wc, 20 + i));
+                fence_proxy_async_global();
+            }
+            const bool one = p.s.kbs == 1;
+            const int copy = p.round_local ? (int)blockIdx.x : 0;
+            for (int r = 0; r < p.s.rounds && ok; ++r) {
+                const int col0 = (blockIdx.x * p.s.rounds + r) * p.s.ct;
+                if (col0 >= p.s.n) break;
+                for (int k = 0; k < p.s.steps; ++k) {
+                    bool there = true;
+                    if (i == 0 || n >= p.s.slots) {
+                        there = ffn_wait(&bars.empty[i][slot], ph ^ 1u, wc, 22 + (int)weights);
+                    } else if (weights) {
+                        // first use of a slot: the newest step of the product before that lies in it.  (Tokens come
+                        // behind the grid barrier, when all of those are done with.)
+                        const SmallShape &o = a.p[0].s;
+                        int j = min(o.slots - 1, ((slot + 1) * p.s.slot_bytes - 1) / o.slot_bytes);
+                        if (j >= rest && slot * p.s.slot_bytes < rest * o.slot_bytes) j = rest - 1;
+                        const int uses = turns + (j < rest ? 1 : 0);
+                        if (uses > 0) there = ffn_wait(&bars.empty[0][j], (uint32_t)(uses - 1) & 1u, wc, 23);
                     }
+                    ok = __all_sync(0xffffffffu, there);
+                    if (!ok) break;
+                    uint64_t *full = &bars.full[i][slot];
+                    const uint32_t dst = smem + slot * p.s.slot_bytes;
+                    if (weights) tma_fill(dst, &p.w, one ? k * kBlock : 0, col0, 0, one ? 0 : k * p.s.kbs, full, (uint32_t)p.s.w_bytes);
+                    else tma_fill(dst + p.s.x_offset, &p.x, one ? k * kBlock : 0, 0, one ? 0 : k * p.s.kbs, copy, full, (uint32_t)p.s.x_bytes);
+                    ++n;
+                    if (++slot == p.s.slots) slot = 0;
+                    if (slot == start) ph ^= 1u;
                 }
             }
-            if (!ok) ffn_linger();
         }
-        __syncwarp();
+        if (!ok) ffn_linger();
     } else if (warp == 2) {
-        if (lane == 0) {
-            int n = 0;
-#pragma unroll          // both products' parameters at fixed places of the constant bank
-            for (int i = 0; i < 2; ++i) {
-                if (i >= a.products || !ok) break;
-                const SmallShape &s = a.p[i].s;
-                const int start = i > 0 ? small_first_slot(a.p[0].s, s, small_steps(a.p[0].s)) : 0;
-                int slot = start;
-                uint32_t ph = 0;
-                const uint32_t idesc = kI8 ? umma_idesc_i8(128, s.kbs * s.box_t) : umma_idesc_bf16(128, s.kbs * s.box_t);
-                for (int r = 0; r < s.rounds && ok; ++r, ++n) {
-                    if ((blockIdx.x * s.rounds + r) * s.ct >= s.n) break;
-                    const int buf = n & 1;
-                    ok = ffn_wait(&bars.acc_empty[buf], ((n >> 1) & 1) ^ 1, wc, 24);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (i >= a.products || !ok) break;
+            const SmallShape &s = a.p[i].s;
+            const int start = i > 0 ? small_first_slot(a.p[0].s, s, small_steps(a.p[0].s)) : 0;
+            int slot = start;
+            uint32_t ph = 0;
+            const uint32_t idesc = kI8 ? umma_idesc_i8(128, s.kbs * s.box_t) : umma_idesc_bf16(128, s.kbs * s.box_t);
+            for (int r = 0; r < s.rounds && ok; ++r, ++n) {
+                if ((blockIdx.x * s.rounds + r) * s.ct >= s.n) break;
+                const int buf = n & 1;
+                ok = __all_sync(0xffffffffu, ffn_wait(&bars.acc_empty[buf], ((n >> 1) & 1) ^ 1, wc, 24));
+                tc_fence_after();
+                for (int k = 0; k < s.steps && ok; ++k) {
+                    ok = __all_sync(0xffffffffu, ffn_wait(&bars.full[i][slot], ph, wc, 25));
+                    if (!ok) break;
                     tc_fence_after();
-                    for (int k = 0; k < s.steps && ok; ++k) {
-                        ok = ffn_wait(&bars.full[i][slot], ph, wc, 25);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t w = smem + slot * s.slot_bytes;
-                        ffn_mma_kstep_one<kI8>(tmem + (uint32_t)(buf * a.acc_cols), umma_desc_sw128(w), umma_desc_sw128(w + s.x_offset), idesc,
-                                               (uint32_t)(k != 0));
-                        tc_commit_one(&bars.empty[i][slot]);
-                        if (++slot == s.slots) slot = 0;
-                        if (slot == start) ph ^= 1u;
-                    }
-                    if (ok) tc_commit_one(&bars.acc_full[buf]);
+                    const uint32_t w = smem + slot * s.slot_bytes;
+                    ffn_mma_kstep_one<kI8>(tmem + (uint32_t)(buf * a.acc_cols), umma_desc_sw128(w), umma_desc_sw128(w + s.x_offset), idesc,
+                                           (uint32_t)(k != 0), &bars.empty[i][slot]);
+                    if (++slot == s.slots) slot = 0;
+                    if (slot == start) ph ^= 1u;
                 }
+                if (ok) tc_commit_one(&bars.acc_full[buf]);
             }
-            if (!ok) ffn_linger();
         }
-        __syncwarp();
+        if (!ok) ffn_linger();
     } else if (warp >= 4) {
         // ---- epilogue: two groups of four warps take turns in blocks of eight tokens; a warp reads the accumulator
         // lanes of its number mod 4
@@ -381,47 +424,46 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
 #pragma unroll
             for (int j = 0; j < 3; ++j) target[j] = small_barrier_target(&a.ctl->barrier[j]);
         int n = 0;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (i >= a.products || !ok) break;
+#pragma unroll 1        // the second product finds these instructions in the cache
+        for (int i = 0; i < a.products && ok; ++i) {
             const SmallProduct &p = a.p[i];
-            const SmallShape &s = p.s;
+            const SmallShape s = p.s;
+            const bool gate = p.gated, out_f32 = p.out_f32;
             if (i > 0) ok = small_grid_barrier(&a.ctl->barrier[0], target[0], ok, wc, 26);
             if constexpr (kI8) {
                 if (ok && p.round_src) {
-                    for (int row = blockIdx.x; row < a.T; row += gridDim.x) {
-                        const int tid256 = threadIdx.x - 128;
-                        if (p.round_f32)
-                            quant_row_by<float, 256, true, true>(static_cast<const float *>(p.round_src), p.round_dst, p.round_scale, row, p.K, tid256,
-                                                                 bars.row_max);
-                        else
-                            quant_row_by<__nv_bfloat16, 256, true, true>(static_cast<const __nv_bfloat16 *>(p.round_src), p.round_dst, p.round_scale,
-                                                                         row, p.K, tid256, bars.row_max);
+                    if (p.round_f32) small_round_rows(static_cast<const float *>(p.round_src), p, a.T, bars.row_max);
+                    else small_round_rows(static_cast<const __nv_bfloat16 *>(p.round_src), p, a.T, bars.row_max);
+                    if (p.round_local) {
+                        fence_proxy_async_global();
                         named_barrier_sync<1, 256>();
+                    } else {
+                        ok = small_grid_barrier(&a.ctl->barrier[1 + i], i == 0 ? target[1] : target[2], ok, wc, 27);
                     }
-                    ok = small_grid_barrier(&a.ctl->barrier[1 + i], i == 0 ? target[1] : target[2], ok, wc, 27);
                 }
             }
             if (!ok) break;
             if (threadIdx.x == 128) mbar_arrive(&bars.tokens[i]);
             if constexpr (kI8) {
                 // (read behind the barriers in the tile's loop)
-                for (int t = threadIdx.x - 128; t < a.T; t += 256) bars.row_scale[t] = __ldcg(p.row_scale + t);
+                const float *scales = p.row_scale + (p.round_local ? (size_t)blockIdx.x * a.T : 0);
+                for (int t = threadIdx.x - 128; t < a.T; t += 256) bars.row_scale[t] = __ldcg(scales + t);
             }
             const int blocks_from = quarter * 32 / s.rows, blocks_to = min(s.kbs - 1, (quarter * 32 + 31) / s.rows), mine = acc_row / s.rows;
-            int pow2 = 1;
-            while (pow2 < s.ct) pow2 *= 2;
             for (int r = 0; r < s.rounds; ++r, ++n) {
                 const int col0 = (blockIdx.x * s.rounds + r) * s.ct;
                 if (col0 >= s.n) break;
                 const int cols = min(s.ct, s.n - col0), buf = n & 1;
-                // a thread's column of the tile, and which of the eight tokens it starts with
-                const int c = tid & (pow2 - 1), t_first = tid / pow2, t_step = 128 / pow2;
-                float sw0 = 0.0f, sw1 = 0.0f;
+                // a thread has one or two items: a column of the tile and the first or second four of eight tokens
+                float sw[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
                 if constexpr (kI8) {
-                    if (c < cols) {
-                        sw0 = p.col_scale[col0 + c];
-                        if (p.gated) sw1 = p.col_scale[s.n + col0 + c];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int item = tid + j * 128, c = item < s.ct ? item : item - s.ct;
+                        if (c < cols) {
+                            sw[j][0] = p.col_scale[col0 + c];
+                            if (gate) sw[j][1] = p.col_scale[s.n + col0 + c];
+                        }
                     }
                 }
                 ok = ffn_wait(&bars.acc_full[buf], (n >> 1) & 1, wc, 28);
@@ -439,38 +481,35 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
                         for (int j = 0; j < 8; ++j) v[j] = b == mine || b == blocks_from ? w[j] : v[j];
                     }
                     if (blocks_from <= blocks_to) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) red[acc_row * 9 + j] = v[j];
+                        uint4 *const to = reinterpret_cast<uint4 *>(red + acc_row * kSmallRedRow);
+                        to[0] = make_uint4(v[0], v[1], v[2], v[3]);
+                        to[1] = make_uint4(v[4], v[5], v[6], v[7]);
                     }
                     if (group == 0) named_barrier_sync<2, 128>();
                     else named_barrier_sync<3, 128>();
-                    const int left = min(8, a.T - t0);
-                    if (c < cols) {
-                        uint8_t *const to = static_cast<uint8_t *>(p.out) + ((long long)(t0 + t_first) * s.n + col0 + c) * (p.out_f32 ? 4 : 2);
-                        const int step_bytes = s.n * t_step * (p.out_f32 ? 4 : 2);
-                        const uint32_t *const from = red + c * 9 + t_first;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int t = t_first + j * t_step;
-                            if (t >= left) break;
-                            const uint32_t *const v = from + j * t_step;
-                            uint32_t sum0 = v[0], sum1 = p.gated ? v[s.ct * 9] : 0u;
-                            for (int b = 1; b < s.kbs; ++b) {
-                                const uint32_t *const w = v + b * s.rows * 9;
-                                if constexpr (kI8) {
-                                    sum0 += w[0];
-                                    if (p.gated) sum1 += w[s.ct * 9];
-                                } else {
-                                    sum0 = __float_as_uint(__uint_as_float(sum0) + __uint_as_float(w[0]));
-                                    if (p.gated) sum1 = __float_as_uint(__uint_as_float(sum1) + __uint_as_float(w[s.ct * 9]));
-                                }
-                            }
-                            const float sx = kI8 ? bars.row_scale[t0 + t] : 0.0f;
-                            float y = small_value<kI8>(sum0, sx, sw0);
-                            if (p.gated) y = gated(y, small_value<kI8>(sum1, sx, sw1));
-                            uint8_t *const at = to + (long long)j * step_bytes;
-                            if (p.out_f32) *reinterpret_cast<float *>(at) = y;
-                            else *reinterpret_cast<__nv_bfloat16 *>(at) = __float2bfloat16_rn(y);
+                    for (int j = 0; j < 2; ++j) {
+                        const int item = tid + j * 128, second = item >= s.ct, c = second ? item - s.ct : item, t = t0 + 4 * second;
+                        if (c >= cols || t >= a.T) continue;
+                        const uint4 *from = reinterpret_cast<const uint4 *>(red + c * kSmallRedRow) + second;
+                        uint4 x = from[0], y = make_uint4(0, 0, 0, 0);
+                        if (gate) y = from[s.ct * (kSmallRedRow / 4)];
+#pragma unroll 1
+                        for (int b = 1; b < s.kbs; ++b) {
+                            from += s.rows * (kSmallRedRow / 4);
+                            x = small_add<kI8>(x, from[0]);
+                            if (gate) y = small_add<kI8>(y, from[s.ct * (kSmallRedRow / 4)]);
+                        }
+                        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+                        const long long at = (long long)t * s.n + col0 + c;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            if (t + q >= a.T) break;
+                            const float sx = kI8 ? bars.row_scale[t + q] : 0.0f;
+                            float f = small_value<kI8>(xs[q], sx, sw[j][0]);
+                            if (gate) f = gated(f, small_value<kI8>(ys[q], sx, sw[j][1]));
+                            if (out_f32) static_cast<float *>(p.out)[at + (long long)q * s.n] = f;
+                            else static_cast<__nv_bfloat16 *>(p.out)[at + (long long)q * s.n] = __float2bfloat16_rn(f);
                         }
                     }
                     if (group == 0) named_barrier_sync<2, 128>();

@@ -12,7 +12,6 @@
 
 namespace weave {
 
-constexpr int kQuantKeep = 8;          // 16-byte vectors of a row that a thread keeps
 constexpr float kQuantMagic = 12582912.0f;      // 1.5 * 2^23: adding it rounds to an integer, in the low bits of the sum
 
 struct QuantRow {
@@ -20,35 +19,31 @@ struct QuantRow {
     bool zero;                         // nothing but zeros: an all-zero row, or one with inf or NaN in it
 };
 
-// The sum's low byte is the integer; it may be one off next to a tie, which the remainder shows: d = x - t s is exact
-// (a multiple of half an ulp of s, below s).
-__device__ __forceinline__ uint32_t quant_guess(float x, const QuantRow &r, bool &close)
+// The sum's low bits are the integer; it may be one off next to a tie, and a tie may have gone the wrong way, which the
+// remainder shows: d = x - t s is exact (a multiple of half an ulp of s, at most about s / 2).
+__device__ __forceinline__ uint32_t quant_guess(float x, const QuantRow &r, float &d)
 {
     const float y = x * r.k;
     const float m = fmaf(y, r.inv, kQuantMagic);
-    close |= fabsf(fmaf(kQuantMagic - m, r.s, y)) >= r.half;
+    d = fmaf(kQuantMagic - m, r.s, y);
     return __float_as_uint(m);
 }
-__device__ __noinline__ uint32_t quant_decide(float x, QuantRow r)
+__device__ __forceinline__ uint32_t quant_mend(uint32_t v, float d, const QuantRow &r)
 {
-    const float y = x * r.k;
-    float t = fmaf(y, r.inv, kQuantMagic) - kQuantMagic;
-    const float d = fmaf(-t, r.s, y);
-    if (fabsf(d) > r.half || (fabsf(d) == r.half && ((int)t & 1))) t += d > 0.0f ? 1.0f : -1.0f;
-    return (uint32_t)(int)fminf(fmaxf(t, -127.0f), 127.0f);        // only rows whose scale is a denormal number reach beyond
+    const float ad = fabsf(d);
+    int t = (int)(v - __float_as_uint(kQuantMagic));
+    if (ad > r.half || (ad == r.half && (t & 1))) t += d > 0.0f ? 1 : -1;
+    return (uint32_t)min(max(t, -127), 127);       // beyond only in a row whose scale is a denormal number
 }
-__device__ __forceinline__ uint32_t quant_four(float a, float b, float c, float d, const QuantRow &r)
+__device__ __forceinline__ uint32_t quant_four(float a, float b, float c, float e, const QuantRow &r)
 {
-    if (r.zero) return 0u;
-    bool close = r.k != 1.0f;
-    uint32_t v[4] = {quant_guess(a, r, close), quant_guess(b, r, close), quant_guess(c, r, close), quant_guess(d, r, close)};
-    if (close) {
-        v[0] = quant_decide(a, r);
-        v[1] = quant_decide(b, r);
-        v[2] = quant_decide(c, r);
-        v[3] = quant_decide(d, r);
+    float d[4];
+    uint32_t v[4] = {quant_guess(a, r, d[0]), quant_guess(b, r, d[1]), quant_guess(c, r, d[2]), quant_guess(e, r, d[3])};
+    if (fmaxf(fmaxf(fabsf(d[0]), fabsf(d[1])), fmaxf(fabsf(d[2]), fabsf(d[3]))) >= r.half || r.k != 1.0f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = quant_mend(v[i], d[i], r);
     }
-    return __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
+    return r.zero ? 0u : __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
 }
 
 __device__ __forceinline__ QuantRow quant_row(uint32_t amax_bits, float &scale)
@@ -89,9 +84,9 @@ __device__ __forceinline__ void quant_put(int8_t *dst, int at, const uint4 &v, c
 }
 
 // One row by kThreads threads (tid from 0), which meet at __syncthreads() or, kNamed, at named barrier 1.  kVec: rows
-// start on 16-byte boundaries and are whole 16-byte vectors long.  `part`: one word of shared memory per warp.  The row
+// start on 16-byte boundaries and are whole 16-byte vectors long.  kKeep: vectors that a thread keeps.  `part`: one word of shared memory per warp.  The row
 // is read past L1, as another SM may just have written it.
-template <class X, int kThreads, bool kVec, bool kNamed>
+template <class X, int kThreads, int kKeep, bool kVec, bool kNamed>
 __device__ __forceinline__ void quant_row_by(const X *x, int8_t *q, float *scale, long long row, int cols, int tid, uint32_t *part)
 {
     const X *src = x + row * cols;
@@ -99,13 +94,14 @@ __device__ __forceinline__ void quant_row_by(const X *x, int8_t *q, float *scale
     const uint4 *vec = reinterpret_cast<const uint4 *>(src);
     const int nv = cols / (int)(16 / sizeof(X));
     uint32_t m = 0;
-    uint4 keep[kQuantKeep];
+    uint4 keep[kKeep];
     if constexpr (kVec) {
 #pragma unroll
-        for (int i = 0; i < kQuantKeep; ++i) keep[i] = tid + i * kThreads < nv ? __ldcg(vec + tid + i * kThreads) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < kKeep; ++i) keep[i] = tid + i * kThreads < nv ? __ldcg(vec + tid + i * kThreads) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < kQuantKeep; ++i) m = quant_max<X>(m, keep[i]);
-        for (int at = tid + kQuantKeep * kThreads; at < nv; at += kThreads) m = quant_max<X>(m, __ldcg(vec + at));
+        for (int i = 0; i < kKeep; ++i) m = quant_max<X>(m, keep[i]);
+#pragma unroll 1
+        for (int at = tid + kKeep * kThreads; at < nv; at += kThreads) m = quant_max<X>(m, __ldcg(vec + at));
         if constexpr (sizeof(X) == 2) m = max(m << 16, m & 0xFFFF0000u);
     } else {
         for (int at = tid; at < cols; at += kThreads) m = max(m, __float_as_uint((float)src[at]) & 0x7FFFFFFFu);
@@ -124,14 +120,27 @@ __device__ __forceinline__ void quant_row_by(const X *x, int8_t *q, float *scale
     const QuantRow r = quant_row(m, s);
     if (tid == 0) scale[row] = s;
     if constexpr (kVec) {
+        // kNamed: a rolled loop that turns the vectors through keep[0].  In a kernel that runs this once, beside a saturated
+        // HBM, it is the fetch of unrolled instructions that takes the time (13 us for a row of 14336 instead of 2)
+        if constexpr (kNamed) {
+#pragma unroll 1
+            for (int at = tid; at < nv && at < kKeep * kThreads; at += kThreads) {
+                quant_put<X>(dst, at, keep[0], r);
 #pragma unroll
-        for (int i = 0; i < kQuantKeep; ++i)
-            if (tid + i * kThreads < nv) quant_put<X>(dst, tid + i * kThreads, keep[i], r);
-        for (int at = tid + kQuantKeep * kThreads; at < nv; at += kThreads) quant_put<X>(dst, at, __ldcg(vec + at), r);
+                for (int i = 1; i < kKeep; ++i) keep[i - 1] = keep[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i)
+                if (tid + i * kThreads < nv) quant_put<X>(dst, tid + i * kThreads, keep[i], r);
+        }
+#pragma unroll 1
+        for (int at = tid + kKeep * kThreads; at < nv; at += kThreads) quant_put<X>(dst, at, __ldcg(vec + at), r);
     } else {
         for (int at = tid; at < cols; at += kThreads) {
-            const float v = (float)src[at];
-            dst[at] = r.zero ? 0 : (int8_t)quant_decide(v, r);
+            float d;
+            const uint32_t v = quant_guess((float)src[at], r, d);
+            dst[at] = r.zero ? 0 : (int8_t)quant_mend(v, d, r);
         }
     }
 }
@@ -143,7 +152,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) weave_quant_kernel(
     __shared__ uint32_t part[kThreads / 32];
     pdl_launch_dependents();
     pdl_wait();
-    quant_row_by<X, kThreads, kVec, false>(x, q, scale, blockIdx.x, cols, threadIdx.x, part);
+    quant_row_by<X, kThreads, 8, kVec, false>(x, q, scale, blockIdx.x, cols, threadIdx.x, part);
 }
 
 }  // namespace weave
