@@ -61,10 +61,10 @@ bool outputs_clear(const Range *out, int n_out, const Range *in, int n_in)
     return true;
 }
 
-template <int kEpi, bool kI8, bool kAMn, bool kBMn>
+template <int kEpi, bool kI8>
 cudaError_t size_gemm()
 {
-    return cudaFuncSetAttribute(weave_gemm_kernel<kEpi, kI8, kAMn, kBMn>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmemBytes);
+    return cudaFuncSetAttribute(weave_gemm_kernel<kEpi, kI8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmemBytes);
 }
 
 template <bool kI8>
@@ -93,10 +93,9 @@ int engine_create(Engine &e, void *workspace)
     err = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &res);
     if (err != cudaSuccess || !fn || res != cudaDriverEntryPointSuccess) return WEAVE_ERR_UNSUPPORTED_DEVICE;
     e.encode = reinterpret_cast<EncodeTiledFn>(fn);
-    if ((err = size_gemm<kEpiStore, false, false, false>()) != cudaSuccess || (err = size_gemm<kEpiStore, false, false, true>()) != cudaSuccess ||
-        (err = size_gemm<kEpiStore, false, true, true>()) != cudaSuccess || (err = size_gemm<kEpiGated, false, false, false>()) != cudaSuccess ||
-        (err = size_gemm<kEpiGrad, false, false, false>()) != cudaSuccess || (err = size_gemm<kEpiScaled, true, false, false>()) != cudaSuccess ||
-        (err = size_gemm<kEpiScaledGated, true, false, false>()) != cudaSuccess || (err = size_small<false>()) != cudaSuccess ||
+    if ((err = size_gemm<kEpiStore, false>()) != cudaSuccess || (err = size_gemm<kEpiGated, false>()) != cudaSuccess ||
+        (err = size_gemm<kEpiGrad, false>()) != cudaSuccess || (err = size_gemm<kEpiScaled, true>()) != cudaSuccess ||
+        (err = size_gemm<kEpiScaledGated, true>()) != cudaSuccess || (err = size_small<false>()) != cudaSuccess ||
         (err = size_small<true>()) != cudaSuccess)
         return cuda_fail(e, err);
     return WEAVE_OK;
@@ -145,10 +144,10 @@ bool map_2d(const Engine &e, CUtensorMap &m, int type, const void *p, long long 
                     box_cols * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// operand whose K runs along the rows' elements: 128 rows x 128 bytes
-bool map_k(const Engine &e, CUtensorMap &m, int type, const void *p, long long rows, long long cols)
+// operand whose K runs along the rows' elements: some rows x 128 bytes
+bool map_k(const Engine &e, CUtensorMap &m, int type, const void *p, long long rows, long long cols, int box_rows = 128)
 {
-    return map_2d(e, m, type, p, rows, cols, 128, type == WEAVE_INT8 ? 128 : 64);
+    return map_2d(e, m, type, p, rows, cols, box_rows, type == WEAVE_INT8 ? 128 : 64);
 }
 // operand whose K runs across the rows (bf16): 64 elements x 64 rows
 bool map_mn(const Engine &e, CUtensorMap &m, const void *p, long long rows, long long cols)
@@ -250,24 +249,62 @@ cudaError_t launch_small(const Engine &e, SmallArgs &a, int T, cudaStream_t stre
     return launch(weave_ffn_small_kernel<kI8>, e.n_sm, kSmallThreads, kSmallSmemMax, kCooperative, stream, a);
 }
 
-template <int kEpi, bool kI8, bool kAMn, bool kBMn>
-cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int M, int N, long long K0, long long K1, LaunchKind kind, cudaStream_t stream)
+// Columns of a tile: the widest, or one that gives idle pairs of SMs work.  A k-step takes the time of its bytes into an
+// SM (94 per ns: 0.35 us for 32 KB), 0.2 us at least; a tile's epilogue is hidden but for the last one's.
+int gemm_width(const Engine &e, int M, int N, int ksteps, int widest, int narrowest, int columns)
 {
-    constexpr int tile_n = kEpi == kEpiStore || kEpi == kEpiScaled ? 256 : 128;
-    constexpr int step = kI8 ? 128 : 64;
+    int best = widest;
+    double best_cost = 1e30;
+    for (int w = widest; w >= narrowest; w /= 2) {
+        const long long tiles = (long long)((M + 255) / 256) * ((N + w - 1) / w), pairs = e.n_sm / 2;
+        const long long waves = (tiles + pairs - 1) / pairs;
+        const double bytes = kGemmHalf + (double)w * columns / 2 * 128, step = bytes / 94000.0 > 0.2 ? bytes / 94000.0 : 0.2;
+        const double epilogue = 0.4 + 0.008 * w * columns;
+        const double tile = ksteps * step > epilogue ? ksteps * step : epilogue, cost = waves * tile + epilogue;
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = w;
+        }
+    }
+    return best;
+}
+
+void gemm_job(GemmJob &j, int M, int N, long long K, int step, int width, bool a_mn, bool b_mn)
+{
+    j.M = M;
+    j.N = N;
+    j.ksteps = (int)((K + step - 1) / step);
+    j.a_mn = a_mn;
+    j.b_mn = b_mn;
+    j.width = width;
+    j.tiles_m = (M + 255) / 256;
+    j.tiles_n = (N + width - 1) / width;
+    j.group_m = 8;
+}
+
+// jobs: of a.job; b_bytes: B's bytes of a k-step in one CTA, at most
+template <int kEpi, bool kI8>
+cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int jobs, int b_bytes, LaunchKind kind, cudaStream_t stream)
+{
     a.ctl = e.ctl;
     a.timeout_ns = e.timeout_ns;
-    a.M = M;
-    a.N = N;
-    a.ksteps[0] = (int)((K0 + step - 1) / step);
-    a.ksteps[1] = (int)((K1 + step - 1) / step);
-    a.b_rank_step = kEpi == kEpiStore || kEpi == kEpiScaled ? 128 : 0;
-    a.tiles_m = (M + 255) / 256;
-    a.tiles_n = (N + tile_n - 1) / tile_n;
-    a.group_m = 8;
-    const long long tiles = (long long)a.tiles_m * a.tiles_n;
-    const int pairs = (int)(tiles < e.n_sm / 2 ? tiles : e.n_sm / 2);
-    return launch(weave_gemm_kernel<kEpi, kI8, kAMn, kBMn>, pairs * 2, kGemmThreads, kGemmSmemBytes, kind, stream, a);
+    a.stage_bytes = kGemmHalf + b_bytes;
+    a.stages = kGemmRing / a.stage_bytes;
+    if (a.stages > kGemmMaxStages) a.stages = kGemmMaxStages;
+    const long long pairs = e.n_sm / 2;
+    long long tiles = 0;
+    for (int i = 0; i < jobs; ++i) tiles += (long long)a.job[i].tiles_m * a.job[i].tiles_n;
+    const int used = (int)(tiles < pairs ? tiles : pairs);
+    a.extra = 0;
+    if (kEpi == kEpiStore) {
+        for (int i = jobs; i < 3; ++i) a.job[i].tiles_m = a.job[i].tiles_n = 0;
+        if (jobs > 1) {
+            // a tile of a few k-steps takes as long as its epilogue, some nine of them
+            const int least = 9, other = a.job[1].ksteps > least ? a.job[1].ksteps : least;
+            a.extra = (a.job[0].ksteps + other / 2) / other;
+        }
+    }
+    return launch(weave_gemm_kernel<kEpi, kI8>, used * 2, kGemmThreads, kGemmSmemBytes, kind, stream, a);
 }
 
 template <class X, int kThreads>
@@ -340,8 +377,6 @@ struct weave_ffn {
     weave_ffn_config cfg;
     FfnLayout L;
     uint8_t *ws;
-    CUtensorMap gate_k, up_k, down_k;          // K along the rows: forward products
-    CUtensorMap gate_up_mn, down_mn;           // K across the rows: backward products
 };
 
 extern "C" {
@@ -368,14 +403,7 @@ int weave_ffn_create(const weave_ffn_config *cfg, weave_ffn_t *out)
     h->L = L;
     h->ws = static_cast<uint8_t *>(cfg->workspace);
     int rc = engine_create(h->e, cfg->workspace);
-    if (rc == WEAVE_OK) {
-        const int H = cfg->hidden, I = cfg->ffn, type = cfg->weight_type;
-        const uint8_t *up = static_cast<const uint8_t *>(cfg->gate_up) + (size_t)I * H * (i8 ? 1 : 2);
-        bool ok = map_k(h->e, h->gate_k, type, cfg->gate_up, I, H) && map_k(h->e, h->up_k, type, up, I, H) &&
-                  map_k(h->e, h->down_k, type, cfg->down, H, I);
-        if (cfg->backward) ok = ok && map_mn(h->e, h->gate_up_mn, cfg->gate_up, 2ll * I, H) && map_mn(h->e, h->down_mn, cfg->down, H, I);
-        rc = ok ? engine_clear(h->e, L.control) : WEAVE_ERR_CUDA;
-    }
+    if (rc == WEAVE_OK) rc = engine_clear(h->e, L.control);
     if (rc != WEAVE_OK) {
         delete h;
         return rc;
@@ -415,26 +443,33 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
         err = i8 ? launch_small<true>(h->e, a, T, stream) : launch_small<false>(h->e, a, T, stream);
         return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
     }
+    // the wide products: gate and up with the activation, then down
     GemmArgs g, d;
-    if (!map_k(h->e, g.a[0], type, left, T, H) || !map_2d(h->e, g.d[0], WEAVE_BF16, hbuf, T, I, 32, 64) ||
-        !map_k(h->e, d.a[0], type, mid, T, I) || !map_2d(h->e, d.d[0], WEAVE_BF16, out, T, H, 32, 64))
+    const int step = i8 ? 128 : 64;
+    const size_t wsize1 = i8 ? 1 : 2;
+    const int wide = gemm_width(h->e, T, I, (H + step - 1) / step, 128, 64, 2), wide_d = gemm_width(h->e, T, H, (I + step - 1) / step, 256, 64, 1);
+    const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * wsize1;
+    if (!map_k(h->e, g.job[0].a, type, left, T, H) || !map_k(h->e, g.job[0].b[0], type, h->cfg.gate_up, I, H, wide) ||
+        !map_k(h->e, g.job[0].b[1], type, up, I, H, wide) || !map_2d(h->e, g.job[0].d, WEAVE_BF16, hbuf, T, I, 32, 64) ||
+        !map_k(h->e, d.job[0].a, type, mid, T, I) || !map_k(h->e, d.job[0].b[0], type, h->cfg.down, H, I, wide_d / 2) ||
+        !map_2d(h->e, d.job[0].d, WEAVE_BF16, out, T, H, 32, 64))
         return WEAVE_ERR_CUDA;
-    g.b[0][0] = h->gate_k;
-    g.b[0][1] = h->up_k;
+    gemm_job(g.job[0], T, I, H, step, wide, false, false);
+    gemm_job(d.job[0], T, H, I, step, wide_d, false, false);
     g.row_scale = xs;
     g.col_scale = h->cfg.gate_up_scale;
-    d.b[0][0] = d.b[0][1] = h->down_k;
+    d.job[0].b[1] = d.job[0].b[0];
     d.row_scale = hs;
     d.col_scale = h->cfg.down_scale;
     d.out_f32 = d.direct = 0;
     if (i8) {
         err = launch_quant(x, WEAVE_BF16, T, H, xq, xs, kPlain, stream);
-        if (err == cudaSuccess) err = launch_gemm<kEpiScaledGated, true, false, false>(h->e, g, T, I, H, 0, kBehind, stream);
+        if (err == cudaSuccess) err = launch_gemm<kEpiScaledGated, true>(h->e, g, 1, wide * 128, kBehind, stream);
         if (err == cudaSuccess) err = launch_quant(hbuf, WEAVE_BF16, T, I, hq, hs, kBehind, stream);
-        if (err == cudaSuccess) err = launch_gemm<kEpiScaled, true, false, false>(h->e, d, T, H, I, 0, kBehind, stream);
+        if (err == cudaSuccess) err = launch_gemm<kEpiScaled, true>(h->e, d, 1, wide_d * 64, kBehind, stream);
     } else {
-        err = launch_gemm<kEpiGated, false, false, false>(h->e, g, T, I, H, 0, kPlain, stream);
-        if (err == cudaSuccess) err = launch_gemm<kEpiStore, false, false, false>(h->e, d, T, H, I, 0, kBehind, stream);
+        err = launch_gemm<kEpiGated, false>(h->e, g, 1, wide * 128, kPlain, stream);
+        if (err == cudaSuccess) err = launch_gemm<kEpiStore, false>(h->e, d, 1, wide_d * 64, kBehind, stream);
     }
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }
@@ -460,38 +495,36 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     uint8_t *hbuf = h->ws + h->L.h, *dgu = h->ws + h->L.dgu;
     // h and [dg du] from x and dy
     GemmArgs g;
-    bool ok = map_k(h->e, g.a[0], WEAVE_BF16, dy, T, H) && map_k(h->e, g.a[1], WEAVE_BF16, x, T, H) &&
-              map_2d(h->e, g.d[0], WEAVE_BF16, hbuf, T, I, 32, 32);
+    const int wide = gemm_width(h->e, T, I, (H + 63) / 64 * 3 / 2, 128, 64, 2);
+    const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * 2;
+    bool ok = map_k(h->e, g.job[0].a, WEAVE_BF16, dy, T, H) && map_mn(h->e, g.job[0].b[0], h->cfg.down, H, I) &&
+              map_k(h->e, g.job[1].a, WEAVE_BF16, x, T, H) && map_k(h->e, g.job[1].b[0], WEAVE_BF16, h->cfg.gate_up, I, H, wide) &&
+              map_k(h->e, g.job[1].b[1], WEAVE_BF16, up, I, H, wide) && map_2d(h->e, g.job[0].d, WEAVE_BF16, hbuf, T, I, 32, 32);
     // d(gate) and d(up) lie side by side in rows of 2I; their maps end where their half ends
     const cuuint64_t dims[2] = {(cuuint64_t)I, (cuuint64_t)T}, strides[1] = {(cuuint64_t)I * 4};
     const cuuint32_t box[2] = {32, 32}, ones[2] = {1, 1};
     for (int half = 0; half < 2 && ok; ++half)
-        ok = h->e.encode(&g.d[1 + half], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dgu + (size_t)half * I * 2, dims, strides, box, ones,
+        ok = h->e.encode(&g.job[1 + half].d, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dgu + (size_t)half * I * 2, dims, strides, box, ones,
                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     if (!ok) return WEAVE_ERR_CUDA;
-    g.b[0][0] = g.b[0][1] = h->down_mn;
-    g.b[1][0] = h->gate_k;
-    g.b[1][1] = h->up_k;
-    err = launch_gemm<kEpiGrad, false, false, false>(h->e, g, T, I, H, H, kPlain, stream);
+    g.job[0].b[1] = g.job[0].b[0];
+    gemm_job(g.job[0], T, I, H, 64, wide, false, false);
+    gemm_job(g.job[1], T, I, H, 64, wide, false, false);
+    err = launch_gemm<kEpiGrad, false>(h->e, g, 1, wide * 128, kPlain, stream);
     if (err != cudaSuccess) return cuda_fail(h->e, err);
-    // dx = [dg du] W_gu
-    if (!map_k(h->e, g.a[0], WEAVE_BF16, dgu, T, 2ll * I) || !map_2d(h->e, g.d[0], WEAVE_BF16, dx, T, H, 32, 64)) return WEAVE_ERR_CUDA;
-    g.b[0][0] = g.b[0][1] = h->gate_up_mn;
-    err = launch_gemm<kEpiStore, false, false, true>(h->e, g, T, H, 2ll * I, 0, kBehind, stream);
-    if (err != cudaSuccess) return cuda_fail(h->e, err);
-    // dW_gu = [dg du]^T x
-    if (!map_mn(h->e, g.a[0], dgu, T, 2ll * I) || !map_mn(h->e, g.b[0][0], x, T, H) ||
-        !map_2d(h->e, g.d[0], WEAVE_BF16, dgate_up, 2ll * I, H, 32, 64))
-        return WEAVE_ERR_CUDA;
-    g.b[0][1] = g.b[0][0];
-    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, 2 * I, H, T, 0, kBehind, stream);
-    if (err != cudaSuccess) return cuda_fail(h->e, err);
-    // dW_d = dy^T h
-    if (!map_mn(h->e, g.a[0], dy, T, H) || !map_mn(h->e, g.b[0][0], hbuf, T, I) || !map_2d(h->e, g.d[0], WEAVE_BF16, ddown, H, I, 32, 64))
-        return WEAVE_ERR_CUDA;
-    g.b[0][1] = g.b[0][0];
-    err = launch_gemm<kEpiStore, false, true, true>(h->e, g, H, I, T, 0, kBehind, stream);
+    // dx = [dg du] W_gu, dW_gu = [dg du]^T x, dW_d = dy^T h: one launch, so that their last waves fill one another
+    GemmArgs d;
+    ok = map_k(h->e, d.job[0].a, WEAVE_BF16, dgu, T, 2ll * I) && map_mn(h->e, d.job[0].b[0], h->cfg.gate_up, 2ll * I, H) &&
+         map_2d(h->e, d.job[0].d, WEAVE_BF16, dx, T, H, 32, 64) && map_mn(h->e, d.job[1].a, dgu, T, 2ll * I) &&
+         map_mn(h->e, d.job[1].b[0], x, T, H) && map_2d(h->e, d.job[1].d, WEAVE_BF16, dgate_up, 2ll * I, H, 32, 64) &&
+         map_mn(h->e, d.job[2].a, dy, T, H) && map_mn(h->e, d.job[2].b[0], hbuf, T, I) && map_2d(h->e, d.job[2].d, WEAVE_BF16, ddown, H, I, 32, 64);
+    if (!ok) return WEAVE_ERR_CUDA;
+    for (int i = 0; i < 3; ++i) d.job[i].b[1] = d.job[i].b[0];
+    gemm_job(d.job[0], T, H, 2ll * I, 64, gemm_width(h->e, T, H, (2 * I + 63) / 64, 256, 128, 1), false, true);
+    gemm_job(d.job[1], 2 * I, H, T, 64, 256, true, true);
+    gemm_job(d.job[2], H, I, T, 64, 256, true, true);
+    err = launch_gemm<kEpiStore, false>(h->e, d, 3, kGemmHalf, kBehind, stream);
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }
 
@@ -542,7 +575,6 @@ struct weave_int8_linear {
     weave_int8_linear_config cfg;
     Int8Layout L;
     uint8_t *ws;
-    CUtensorMap weight_k;
 };
 
 extern "C" {
@@ -579,9 +611,7 @@ int weave_int8_linear_create(const weave_int8_linear_config *cfg, weave_int8_lin
     h->L = L;
     h->ws = static_cast<uint8_t *>(cfg->workspace);
     int rc = engine_create(h->e, cfg->workspace);
-    if (rc == WEAVE_OK)
-        rc = map_k(h->e, h->weight_k, WEAVE_INT8, cfg->weight, cfg->out_features, cfg->in_features) ? engine_clear(h->e, L.control)
-                                                                                                    : WEAVE_ERR_CUDA;
+    if (rc == WEAVE_OK) rc = engine_clear(h->e, L.control);
     if (rc != WEAVE_OK) {
         delete h;
         return rc;
@@ -627,16 +657,18 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
         if (err != cudaSuccess) return cuda_fail(h->e, err);
     }
     GemmArgs g;
+    const int wide = gemm_width(h->e, T, N, (K + 127) / 128, 256, 64, 1);
     g.direct = (size_t)N * out_size % 16 != 0;
     g.out_f32 = out_type == WEAVE_F32;
     g.out = out;
     g.ld_out = N;
     g.row_scale = x_scale;
     g.col_scale = h->cfg.scale;
-    if (!map_k(h->e, g.a[0], WEAVE_INT8, q, T, K)) return WEAVE_ERR_CUDA;
-    if (!g.direct && !map_2d(h->e, g.d[0], out_type, out, T, N, 32, out_type == WEAVE_F32 ? 32 : 64)) return WEAVE_ERR_CUDA;
-    g.b[0][0] = g.b[0][1] = h->weight_k;
-    err = launch_gemm<kEpiScaled, true, false, false>(h->e, g, T, N, K, 0, round ? kBehind : kPlain, stream);
+    if (!map_k(h->e, g.job[0].a, WEAVE_INT8, q, T, K) || !map_k(h->e, g.job[0].b[0], WEAVE_INT8, h->cfg.weight, N, K, wide / 2)) return WEAVE_ERR_CUDA;
+    if (!g.direct && !map_2d(h->e, g.job[0].d, out_type, out, T, N, 32, out_type == WEAVE_F32 ? 32 : 64)) return WEAVE_ERR_CUDA;
+    g.job[0].b[1] = g.job[0].b[0];
+    gemm_job(g.job[0], T, N, K, 128, wide, false, false);
+    err = launch_gemm<kEpiScaled, true>(h->e, g, 1, wide * 64, round ? kBehind : kPlain, stream);
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }
 

@@ -9,8 +9,8 @@
 //   kEpiScaled      D = (A B) * (row scale * column scale) in bf16 or fp32 (256)         8-bit integers, K-major
 //   kEpiScaledGated h as above from scaled g and u (128)                                 8-bit integers, K-major
 //
-// A tile is 256 rows of A (128 per CTA) by 256 accumulator columns.  A k-step is 128 bytes of K (64 bf16 or 128
-// 8-bit integers): 16 KB of A and 16 KB of B per CTA, six of them in flight.  Rows, columns and K that stick out over
+// A tile is 256 rows of A (128 per CTA) by up to 256 accumulator columns (fewer where that gives idle SMs work).  A k-step
+// is 128 bytes of K (64 bf16 or 128 8-bit integers): 16 KB of A and up to 16 KB of B per CTA, 192 KB of them in flight.  Rows, columns and K that stick out over
 // the matrices are zero-filled by the tensor maps on the way in and clipped by them on the way out.
 //
 // Bound: the tensor pipe (256 x 256 x 16 takes 128 cycles) and, over more than some milliseconds, the power limit.
@@ -138,53 +138,93 @@ __device__ __forceinline__ float gated(float g, float u) { return g * fast_sigmo
 
 // ------------------------------------------------------------------------------------ the kernel
 
+// One product.  kEpiGrad has two over the same tiles, job 0 for dh and job 1 for g and u; kEpiStore up to three
+// independent ones in one launch; the other forms have one.
+struct alignas(64) GemmJob {
+    CUtensorMap a;
+    CUtensorMap b[2];        // [rank of the CTA in its pair]: the gated forms give gate rows to one, up rows to the other
+    CUtensorMap d;           // results; kEpiGrad: h, dg, du in jobs 0, 1, 2
+    int M, N;                // rows and columns of the result
+    int ksteps;
+    int a_mn, b_mn;          // kEpiStore: operand is MN-major
+    int width;               // columns of the result in a tile
+    int tiles_m, tiles_n, group_m;
+};
+
 struct alignas(64) GemmArgs {
-    CUtensorMap a[2];        // [phase]; phase 1 only in kEpiGrad
-    CUtensorMap b[2][2];     // [phase][rank of the CTA in its pair]: the gated forms give gate rows to one, up rows to the other
-    CUtensorMap d[3];        // results: D or h, dg, du
+    GemmJob job[3];
     FfnCtl *ctl;
     unsigned long long timeout_ns;
     const float *row_scale;  // scaled forms: [M] and [N] (gated: [2N], gate then up)
     const float *col_scale;
     void *out;               // kEpiScaled, for rows that no tensor map can describe
     long long ld_out;
-    int M, N;                // rows and columns of the result
-    int ksteps[2];
-    int b_rank_step;         // columns between the two CTAs' parts of B in phase 1 (0 where the maps differ instead)
-    int tiles_m, tiles_n, group_m;
     int out_f32, direct;     // kEpiScaled: type of the result; 1 = ordinary stores (row length not a multiple of 16 bytes)
+    int extra;               // kEpiStore: see gemm_tile()
+    int stages, stage_bytes;
 };
 
 constexpr int kGemmThreads = 256;
-constexpr int kGemmStages = 6;
-constexpr int kGemmHalf = 16384;                    // one operand's bytes of one k-step in one CTA
-constexpr int kGemmStage = 2 * kGemmHalf;
+constexpr int kGemmMaxStages = 9;
+constexpr int kGemmHalf = 16384;                    // A's bytes of one k-step in one CTA, B's at most
+constexpr int kGemmRing = 6 * 2 * kGemmHalf;
 constexpr int kGemmStaging = 8192;                  // per epilogue warp
-constexpr int kGemmSmemStaging = kGemmStages * kGemmStage;
+constexpr int kGemmSmemStaging = kGemmRing;
 constexpr int kGemmSmemScales = kGemmSmemStaging + 4 * kGemmStaging;
 constexpr int kGemmSmemBars = kGemmSmemScales + 4 * 256;
 constexpr int kGemmSmemBytes = kGemmSmemBars + 256 + 1024;      // 1024: the stages start on a swizzle atom's boundary
 static_assert(kGemmSmemBytes <= 232448, "227 KB per CTA");
 
 struct GemmBars {
-    uint64_t full[kGemmStages], empty[kGemmStages];
+    uint64_t full[kGemmMaxStages], empty[kGemmMaxStages];
     uint64_t acc_full[2], acc_empty[2];
     uint32_t tmem_base;
 };
+static_assert(sizeof(GemmBars) <= 256, "the barriers' place in shared memory");
 
-// Tiles in groups of group_m row tiles, all columns of a group before the next group, row tiles fastest: the pairs at
-// work at one time share a few panels of B and the group's rows of A in L2.
-__device__ __forceinline__ void tile_at(const GemmArgs &p, int t, int &m0, int &n0, int tile_n)
+struct GemmTile { int job, m0, n0; };
+
+// Tiles of a job in groups of group_m row tiles, all columns of a group before the next group, row tiles fastest: the
+// pairs at work at one time share a few panels of B and the group's rows of A in L2.
+__device__ __forceinline__ void gemm_tile_at(const GemmJob &p, int t, GemmTile &at)
 {
     const int per = p.group_m * p.tiles_n;
     const int g = t / per, r = t - g * per;
     const int gm = min(p.group_m, p.tiles_m - g * p.group_m);
     const int n = r / gm;
-    m0 = (g * p.group_m + r - n * gm) * 256;
-    n0 = n * tile_n;
+    at.m0 = (g * p.group_m + r - n * gm) * 256;
+    at.n0 = n * p.width;
 }
 
-template <int kEpi, bool kI8, bool kAMn, bool kBMn>
+// The i-th tile of a CTA pair; false behind its last.  Job 0's tiles go round the pairs; the pairs that get one less of
+// them take `extra` tiles of jobs 1 and 2 for it (as many as cost the same), whose remaining ones go round all pairs.
+template <bool kJobs>
+__device__ __forceinline__ bool gemm_tile(const GemmArgs &p, int i, int pair, int pairs, GemmTile &at)
+{
+    const int n0 = p.job[0].tiles_m * p.job[0].tiles_n;
+    int t = pair + i * pairs;
+    at.job = 0;
+    if constexpr (kJobs) {
+        if (t >= n0) {
+            const int n1 = p.job[1].tiles_m * p.job[1].tiles_n, n2 = p.job[2].tiles_m * p.job[2].tiles_n;
+            const int rest = n0 % pairs, few = rest ? pairs - rest : 0;
+            const int j = i - (n0 > pair ? (n0 - pair + pairs - 1) / pairs : 0);
+            if (few == 0 || pair < rest) t = few * p.extra + j * pairs + pair;
+            else if (j < p.extra) t = j * few + pair - rest;
+            else t = few * p.extra + (j - p.extra) * pairs + pair;
+            if (t >= n1 + n2) return false;
+            at.job = t < n1 ? 1 : 2;
+            if (t >= n1) t -= n1;
+            gemm_tile_at(p.job[at.job], t, at);
+            return true;
+        }
+    }
+    if (t >= n0) return false;
+    gemm_tile_at(p.job[0], t, at);
+    return true;
+}
+
+template <int kEpi, bool kI8>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) weave_gemm_kernel(const __grid_constant__ GemmArgs p)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -194,16 +234,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int tiles = p.tiles_m * p.tiles_n;
     const WaitCtx wc = {p.ctl, p.timeout_ns};
     constexpr bool kGatedTile = kEpi == kEpiGated || kEpi == kEpiGrad || kEpi == kEpiScaledGated;
-    constexpr int kTileN = kGatedTile ? 128 : 256;
+    constexpr bool kJobs = kEpi == kEpiStore;
     constexpr int kPhases = kEpi == kEpiGrad ? 2 : 1;
     constexpr int kStepK = kI8 ? 128 : 64;          // elements of K in a k-step
+    GemmTile at;
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kGemmStages; ++i) { mbar_init(&bars.full[i], 1); mbar_init(&bars.empty[i], 1); }
+        for (int i = 0; i < kGemmMaxStages; ++i) { mbar_init(&bars.full[i], 1); mbar_init(&bars.empty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&bars.acc_full[i], 1); mbar_init(&bars.acc_empty[i], 8); }
         fence_mbar_init();
     }
@@ -222,34 +262,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
         pdl_wait();
         int s = 0;
         uint32_t ph = 0;
-        for (int t = pair; t < tiles && ok; t += pairs) {
-            int m0, n0;
-            tile_at(p, t, m0, n0, kTileN);
+        for (int i = 0; ok && gemm_tile<kJobs>(p, i, pair, pairs, at); ++i) {
             for (int phase = 0; phase < kPhases && ok; ++phase) {
-                const bool first_of_two = kPhases == 2 && phase == 0;
-                const bool b_mn = kEpi == kEpiGrad ? phase == 0 : kBMn;
-                const void *map = load_a ? &p.a[phase] : &p.b[phase][rank];
-                const int mn = load_a ? m0 + (int)rank * 128
-                                      : first_of_two ? n0 + (int)rank * 64 : n0 + (int)rank * p.b_rank_step;
-                const bool mn_major = load_a ? kAMn : b_mn;
-                const uint32_t tx = first_of_two ? 2u * (kGemmHalf + kGemmHalf / 2) : 2u * kGemmStage;
-                const int ks = p.ksteps[phase];
+                const GemmJob &job = p.job[kPhases == 2 ? phase : at.job];
+                const bool dh = kPhases == 2 && phase == 0;
+                const bool a_mn = kJobs && job.a_mn, b_mn = kJobs ? job.b_mn != 0 : dh;
+                const int half = kGatedTile && !dh ? job.width : job.width / 2;          // this CTA's rows of B
+                const int b_boxes = b_mn ? (half + 63) / 64 : 1;
+                const uint32_t tx = 2u * (kGemmHalf + (b_mn ? (uint32_t)b_boxes * 8192u : (uint32_t)half * 128u));
+                const void *map = load_a ? &job.a : &job.b[rank];
+                const int mn = load_a ? at.m0 + (int)rank * 128 : at.n0 + (kGatedTile && !dh ? 0 : (int)rank * half);
+                const bool mn_major = load_a ? a_mn : b_mn;
+                const bool second = load_a ? a_mn : b_boxes == 2;
+                const int ks = job.ksteps;
                 for (int k = 0; k < ks; ++k) {
                     ok = __all_sync(0xffffffffu, ffn_wait(&bars.empty[s], ph ^ 1u, wc, 1 + warp));
                     if (!ok) break;
-                    const uint32_t dst = smem + s * kGemmStage + (load_a ? 0 : kGemmHalf);
+                    const uint32_t dst = smem + s * p.stage_bytes + (load_a ? 0 : kGemmHalf);
                     const uint32_t full = mapa_u32(smem_u32(&bars.full[s]), 0);
                     if (elect_one()) {
                         if (load_a && rank == 0) mbar_arrive_expect_tx(&bars.full[s], tx);
-                        if (mn_major) {
-                            tma_load_2d_pair(dst, map, mn, k * kStepK, full);
-                            if (!first_of_two || load_a) tma_load_2d_pair(dst + 8192, map, mn + 64, k * kStepK, full);
-                        } else {
-                            tma_load_2d_pair(dst, map, k * kStepK, mn, full);
-                        }
+                        tma_load_2d_pair(dst, map, mn_major ? mn : k * kStepK, mn_major ? k * kStepK : mn, full);
+                        if (second) tma_load_2d_pair(dst + 8192, map, mn + 64, k * kStepK, full);
                     }
                     __syncwarp();
-                    if (++s == kGemmStages) { s = 0; ph ^= 1u; }
+                    if (++s == p.stages) { s = 0; ph ^= 1u; }
                 }
             }
         }
@@ -257,36 +294,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
     } else if (warp == 2) {
         if (rank == 0) {
             // ---- the pair's issuer
-            const uint32_t idesc256 = (kI8 ? umma_idesc_i8(256, 256) : umma_idesc_bf16(256, 256)) | (kAMn ? kIdescAMn : 0u) |
-                                      (kBMn ? kIdescBMn : 0u);
-            const uint32_t idesc_dh = umma_idesc_bf16(256, 128) | kIdescBMn;
-            const uint64_t a_inc = kAMn ? 128 : 2;
-            int s = 0, n = 0;
+            int s = 0;
             uint32_t ph = 0;
-            for (int t = pair; t < tiles && ok; t += pairs, ++n) {
+            for (int n = 0; ok && gemm_tile<kJobs>(p, n, pair, pairs, at); ++n) {
                 // kEpiGrad: g and u in columns 0-255, dh in 256-383 or 384-511: the next tile's dh is summed up
                 // while the epilogue still reads this one's
                 const int buf = n & 1;
                 if (kEpi != kEpiGrad) ok = __all_sync(0xffffffffu, ffn_wait(&bars.acc_empty[buf], ((n >> 1) & 1) ^ 1, wc, 3));
                 for (int phase = 0; phase < kPhases && ok; ++phase) {
+                    const GemmJob &job = p.job[kPhases == 2 ? phase : at.job];
                     const bool dh = kPhases == 2 && phase == 0;
                     if (kPhases == 2 && phase == 1) {
                         ok = __all_sync(0xffffffffu, ffn_wait(&bars.acc_empty[0], (n & 1) ^ 1, wc, 3));
                         if (!ok) break;
                     }
                     tc_fence_after();
+                    const bool a_mn = kJobs && job.a_mn, b_mn = kJobs ? job.b_mn != 0 : dh;
                     const uint32_t d = tmem + (kEpi != kEpiGrad ? buf * 256 : dh ? 256 + buf * 128 : 0);
-                    const bool b_mn = kEpi == kEpiGrad ? dh : kBMn;
-                    const int ks = p.ksteps[phase];
+                    const uint32_t n_mma = (uint32_t)(kGatedTile && !dh ? 2 * job.width : job.width);
+                    const uint32_t idesc = (kI8 ? umma_idesc_i8(256, n_mma) : umma_idesc_bf16(256, n_mma)) | (a_mn ? kIdescAMn : 0u) |
+                                           (b_mn ? kIdescBMn : 0u);
+                    const uint64_t a_inc = a_mn ? 128 : 2, b_inc = b_mn ? 128 : 2;
+                    const int ks = job.ksteps;
                     for (int k = 0; k < ks; ++k) {
                         ok = __all_sync(0xffffffffu, ffn_wait(&bars.full[s], ph, wc, 4));
                         if (!ok) break;
                         tc_fence_after();
-                        const uint32_t a = smem + s * kGemmStage, b = a + kGemmHalf;
-                        ffn_mma_kstep_pair<kI8>(d, kAMn ? umma_desc_mn_sw128(a) : umma_desc_sw128(a),
-                                                b_mn ? umma_desc_mn_sw128(b) : umma_desc_sw128(b), a_inc, b_mn ? 128 : 2,
-                                                dh ? idesc_dh : idesc256, (uint32_t)(k != 0), &bars.empty[s]);
-                        if (++s == kGemmStages) { s = 0; ph ^= 1u; }
+                        const uint32_t a = smem + s * p.stage_bytes, b = a + kGemmHalf;
+                        ffn_mma_kstep_pair<kI8>(d, a_mn ? umma_desc_mn_sw128(a) : umma_desc_sw128(a),
+                                                b_mn ? umma_desc_mn_sw128(b) : umma_desc_sw128(b), a_inc, b_inc, idesc, (uint32_t)(k != 0),
+                                                &bars.empty[s]);
+                        if (++s == p.stages) { s = 0; ph ^= 1u; }
                     }
                 }
                 if (ok && elect_one()) tc_commit_pair(&bars.acc_full[buf], 3);
@@ -302,32 +340,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
         float *const scales = reinterpret_cast<float *>(smem_g + kGemmSmemScales + quarter * 256);
         const uint32_t empty0 = mapa_u32(smem_u32(&bars.acc_empty[0]), 0);
         pdl_wait();
-        int n = 0;
-        uint32_t slot = 0;          // kEpiStore, kEpiScaled in bf16: half of the staging buffer that is written next
-        for (int t = pair; t < tiles; t += pairs, ++n) {
-            int m0, n0;
-            tile_at(p, t, m0, n0, kTileN);
-            const int row0 = m0 + (int)rank * 128 + quarter * 32;
+        uint32_t slot = 0;          // half of the staging buffer that is written next (not kEpiGrad)
+        for (int n = 0; gemm_tile<kJobs>(p, n, pair, pairs, at); ++n) {
+            const GemmJob &job = p.job[at.job];
+            const int M = job.M, N = job.N, width = job.width, n0 = at.n0;
+            const int row0 = at.m0 + (int)rank * 128 + quarter * 32;
             const int buf = n & 1;
             ok = __all_sync(0xffffffffu, ffn_wait(&bars.acc_full[buf], (n >> 1) & 1, wc, 5));
             if (!ok) break;
             tc_fence_after();
-            const bool any_row = row0 < p.M;       // whole warp
+            const bool any_row = row0 < M;       // whole warp
             float sx = 0.0f;
-            if constexpr (kI8) sx = row0 + lane < p.M ? p.row_scale[row0 + lane] : 0.0f;
+            if constexpr (kI8) sx = row0 + lane < M ? p.row_scale[row0 + lane] : 0.0f;
 
             if constexpr (kEpi == kEpiStore || kEpi == kEpiScaled) {
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < width / 64; ++c) {
                     const int col = n0 + c * 64;
                     uint32_t v[64];
                     tmem_ld_32x64(lane_base + buf * 256 + c * 64, v);
                     tmem_ld_wait64(v);
-                    if (!any_row || col >= p.N) continue;
+                    if (!any_row || col >= N) continue;
                     if constexpr (kEpi == kEpiScaled) {
                         __syncwarp();
-                        scales[lane] = col + lane < p.N ? p.col_scale[col + lane] : 0.0f;
-                        scales[lane + 32] = col + 32 + lane < p.N ? p.col_scale[col + 32 + lane] : 0.0f;
+                        scales[lane] = col + lane < N ? p.col_scale[col + lane] : 0.0f;
+                        scales[lane + 32] = col + 32 + lane < N ? p.col_scale[col + 32 + lane] : 0.0f;
                         __syncwarp();
 #pragma unroll
                         for (int i = 0; i < 64; i += 4) {
@@ -350,8 +387,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                             for (int i = 0; i < 32; ++i) st_shared_u32(stage + lane * 132 + i * 4, v[half * 32 + i]);
                             __syncwarp();
                             const int cc = col + half * 32 + lane;
-                            const int rows = min(32, p.M - row0);
-                            if (cc < p.N)
+                            const int rows = min(32, M - row0);
+                            if (cc < N)
                                 for (int r = 0; r < rows; ++r) {
                                     const float y = ld_shared_f32(stage + r * 132 + lane * 4);
                                     const long long at = (long long)(row0 + r) * p.ld_out + cc;
@@ -375,7 +412,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                                                         v[half * 32 + j * 4 + 3]));
                             fence_proxy_async_shared();
                             __syncwarp();
-                            if (lane == 0 && col + half * 32 < p.N) tma_store_2d(&p.d[0], dst, col + half * 32, row0);
+                            if (lane == 0 && col + half * 32 < N) tma_store_2d(&job.d, dst, col + half * 32, row0);
                             if (lane == 0) bulk_commit();
                         }
                     } else {
@@ -393,13 +430,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                         }
                         fence_proxy_async_shared();
                         __syncwarp();
-                        if (lane == 0) { tma_store_2d(&p.d[0], dst, col, row0); bulk_commit(); }
+                        if (lane == 0) { tma_store_2d(&job.d, dst, col, row0); bulk_commit(); }
                     }
                 }
             } else if constexpr (kEpi == kEpiGated || kEpi == kEpiScaledGated) {
 #pragma unroll 1
-                for (int c = 0; c < 2; ++c) {
-                    const uint32_t dst = stage + c * 4096;
+                for (int c = 0; c < width / 64; ++c) {
+                    const uint32_t dst = stage + slot * 4096;
+                    slot ^= 1u;
                     if (lane == 0) bulk_wait_read<1>();
                     __syncwarp();
 #pragma unroll
@@ -407,14 +445,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                         const int cc = c * 64 + half * 32;
                         uint32_t g[32], u[32];
                         tmem_ld_32x32(lane_base + buf * 256 + cc, g);
-                        tmem_ld_32x32(lane_base + buf * 256 + 128 + cc, u);
+                        tmem_ld_32x32(lane_base + buf * 256 + width + cc, u);
                         tmem_ld_wait32(g);
                         reg_fence32(u);
                         if constexpr (kEpi == kEpiScaledGated) {
                             const int col = n0 + cc + lane;
                             __syncwarp();
-                            scales[lane] = col < p.N ? p.col_scale[col] : 0.0f;
-                            scales[lane + 32] = col < p.N ? p.col_scale[p.N + col] : 0.0f;
+                            scales[lane] = col < N ? p.col_scale[col] : 0.0f;
+                            scales[lane + 32] = col < N ? p.col_scale[N + col] : 0.0f;
                             __syncwarp();
 #pragma unroll
                             for (int i = 0; i < 32; i += 4) {
@@ -443,7 +481,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                     fence_proxy_async_shared();
                     __syncwarp();
                     if (lane == 0) {
-                        if (any_row && n0 + c * 64 < p.N) tma_store_2d(&p.d[0], dst, n0 + c * 64, row0);
+                        if (any_row && n0 + c * 64 < N) tma_store_2d(&job.d, dst, n0 + c * 64, row0);
                         bulk_commit();
                     }
                 }
@@ -452,10 +490,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                 // of the staging buffer
                 int quad = 0;
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < width / 32; ++c) {
                     uint32_t g[32], u[32], d[32];
                     tmem_ld_32x32(lane_base + c * 32, g);
-                    tmem_ld_32x32(lane_base + 128 + c * 32, u);
+                    tmem_ld_32x32(lane_base + width + c * 32, u);
                     tmem_ld_32x32(lane_base + 256 + buf * 128 + c * 32, d);
                     tmem_ld_wait32(g);
                     reg_fence32(u);
@@ -487,7 +525,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                         fence_proxy_async_shared();
                         __syncwarp();
                         if (lane == 0) {
-                            if (any_row && n0 + c * 32 < p.N) tma_store_2d(&p.d[which], dst, n0 + c * 32, row0);
+                            if (any_row && n0 + c * 32 < N) tma_store_2d(&p.job[which].d, dst, n0 + c * 32, row0);
                             bulk_commit();
                         }
                     }
