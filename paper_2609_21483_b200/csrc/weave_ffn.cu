@@ -141,7 +141,9 @@ bool map_2d(const Engine &e, CUtensorMap &m, int type, const void *p, long long 
                                    : type == WEAVE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                                        : CU_TENSOR_MAP_DATA_TYPE_UINT8;
     return e.encode(&m, dt, 2, const_cast<void *>(p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    box_cols * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                    box_cols * size == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
+                    : box_cols * size == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                            : CU_TENSOR_MAP_SWIZZLE_NONE,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // operand whose K runs along the rows' elements: some rows x 128 bytes
@@ -249,18 +251,40 @@ cudaError_t launch_small(const Engine &e, SmallArgs &a, int T, cudaStream_t stre
     return launch(weave_ffn_small_kernel<kI8>, e.n_sm, kSmallThreads, kSmallSmemMax, kCooperative, stream, a);
 }
 
-// Columns of a tile: the widest, or one that gives idle pairs of SMs work.  A k-step takes the time of its bytes into an
-// SM (94 per ns: 0.35 us for 32 KB), 0.2 us at least; a tile's epilogue is hidden but for the last one's.
-int gemm_width(const Engine &e, int M, int N, int ksteps, int widest, int narrowest, int columns)
+// Columns of a tile (a multiple of `unit`; each takes `columns` of the accumulator's): as narrow as the number of waves
+// over the pairs of SMs allows, and rather more waves of narrower tiles than idle pairs.  A k-step takes the time of its
+// bytes into an SM (94 per ns: 0.35 us for 32 KB), 0.2 us at least; a tile's epilogue is hidden but for the last one's.
+double gemm_tile_us(int ksteps, int accumulator_columns)
+{
+    const double bytes = kGemmHalf + accumulator_columns * 64.0, step = bytes / 94000.0 > 0.2 ? bytes / 94000.0 : 0.2;
+    const double epilogue = 0.4 + 0.008 * accumulator_columns;
+    return ksteps * step > epilogue ? ksteps * step : epilogue;
+}
+long long gemm_tiles(int M, int N, int width) { return (long long)((M + 255) / 256) * ((N + width - 1) / width); }
+int gemm_width(const Engine &e, int M, int N, int ksteps, int widest, int unit, int columns)
 {
     int best = widest;
     double best_cost = 1e30;
-    for (int w = widest; w >= narrowest; w /= 2) {
-        const long long tiles = (long long)((M + 255) / 256) * ((N + w - 1) / w), pairs = e.n_sm / 2;
-        const long long waves = (tiles + pairs - 1) / pairs;
-        const double bytes = kGemmHalf + (double)w * columns / 2 * 128, step = bytes / 94000.0 > 0.2 ? bytes / 94000.0 : 0.2;
-        const double epilogue = 0.4 + 0.008 * w * columns;
-        const double tile = ksteps * step > epilogue ? ksteps * step : epilogue, cost = waves * tile + epilogue;
+    for (int w = widest; w * columns >= 64 && w > 0; w -= unit) {
+        const long long pairs = e.n_sm / 2, waves = (gemm_tiles(M, N, w) + pairs - 1) / pairs;
+        const double cost = waves * gemm_tile_us(ksteps, w * columns) + 0.008 * w * columns;
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = w;
+        }
+    }
+    return best;
+}
+// ... of the long product in a launch with others, which fill the pairs that it leaves: the longer of its own waves and
+// of all work spread evenly.  (dx of T = 777, 1096 x 2744, all three products, us with 256, 128, 64 columns: 40, 32, 52.)
+int gemm_width_among(const Engine &e, int M, int N, int ksteps, double others_us)
+{
+    int best = 256;
+    double best_cost = 1e30;
+    for (int w = 256; w >= 64; w -= 64) {
+        const long long pairs = e.n_sm / 2, tiles = gemm_tiles(M, N, w), waves = (tiles + pairs - 1) / pairs;
+        const double tile = gemm_tile_us(ksteps, w), own = waves * tile, even = (tiles * tile + others_us) / pairs;
+        const double cost = own > even ? own : even;
         if (cost < best_cost) {
             best_cost = cost;
             best = w;
@@ -282,6 +306,12 @@ void gemm_job(GemmJob &j, int M, int N, long long K, int step, int width, bool a
     j.group_m = 8;
 }
 
+// a result in bf16
+bool map_d(const Engine &e, GemmJob &j, const void *p, long long rows, long long cols)
+{
+    return map_2d(e, j.d, WEAVE_BF16, p, rows, cols, 32, 64) && map_2d(e, j.d8, WEAVE_BF16, p, rows, cols, 32, 8);
+}
+
 // jobs: of a.job; b_bytes: B's bytes of a k-step in one CTA, at most
 template <int kEpi, bool kI8>
 cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int jobs, int b_bytes, LaunchKind kind, cudaStream_t stream)
@@ -299,9 +329,7 @@ cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int jobs, int b_bytes, Lau
     if (kEpi == kEpiStore) {
         for (int i = jobs; i < 3; ++i) a.job[i].tiles_m = a.job[i].tiles_n = 0;
         if (jobs > 1) {
-            // a tile of a few k-steps takes as long as its epilogue, some nine of them
-            const int least = 9, other = a.job[1].ksteps > least ? a.job[1].ksteps : least;
-            a.extra = (a.job[0].ksteps + other / 2) / other;
+            a.extra = (int)(gemm_tile_us(a.job[0].ksteps, a.job[0].width) / gemm_tile_us(a.job[1].ksteps, a.job[1].width) + 0.5);
         }
     }
     return launch(weave_gemm_kernel<kEpi, kI8>, used * 2, kGemmThreads, kGemmSmemBytes, kind, stream, a);
@@ -447,12 +475,12 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     GemmArgs g, d;
     const int step = i8 ? 128 : 64;
     const size_t wsize1 = i8 ? 1 : 2;
-    const int wide = gemm_width(h->e, T, I, (H + step - 1) / step, 128, 64, 2), wide_d = gemm_width(h->e, T, H, (I + step - 1) / step, 256, 64, 1);
+    const int wide = gemm_width(h->e, T, I, (H + step - 1) / step, 128, 8, 2), wide_d = gemm_width(h->e, T, H, (I + step - 1) / step, 256, 16, 1);
     const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * wsize1;
     if (!map_k(h->e, g.job[0].a, type, left, T, H) || !map_k(h->e, g.job[0].b[0], type, h->cfg.gate_up, I, H, wide) ||
-        !map_k(h->e, g.job[0].b[1], type, up, I, H, wide) || !map_2d(h->e, g.job[0].d, WEAVE_BF16, hbuf, T, I, 32, 64) ||
+        !map_k(h->e, g.job[0].b[1], type, up, I, H, wide) || !map_d(h->e, g.job[0], hbuf, T, I) ||
         !map_k(h->e, d.job[0].a, type, mid, T, I) || !map_k(h->e, d.job[0].b[0], type, h->cfg.down, H, I, wide_d / 2) ||
-        !map_2d(h->e, d.job[0].d, WEAVE_BF16, out, T, H, 32, 64))
+        !map_d(h->e, d.job[0], out, T, H))
         return WEAVE_ERR_CUDA;
     gemm_job(g.job[0], T, I, H, step, wide, false, false);
     gemm_job(d.job[0], T, H, I, step, wide_d, false, false);
@@ -516,12 +544,13 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     // dx = [dg du] W_gu, dW_gu = [dg du]^T x, dW_d = dy^T h: one launch, so that their last waves fill one another
     GemmArgs d;
     ok = map_k(h->e, d.job[0].a, WEAVE_BF16, dgu, T, 2ll * I) && map_mn(h->e, d.job[0].b[0], h->cfg.gate_up, 2ll * I, H) &&
-         map_2d(h->e, d.job[0].d, WEAVE_BF16, dx, T, H, 32, 64) && map_mn(h->e, d.job[1].a, dgu, T, 2ll * I) &&
-         map_mn(h->e, d.job[1].b[0], x, T, H) && map_2d(h->e, d.job[1].d, WEAVE_BF16, dgate_up, 2ll * I, H, 32, 64) &&
-         map_mn(h->e, d.job[2].a, dy, T, H) && map_mn(h->e, d.job[2].b[0], hbuf, T, I) && map_2d(h->e, d.job[2].d, WEAVE_BF16, ddown, H, I, 32, 64);
+         map_d(h->e, d.job[0], dx, T, H) && map_mn(h->e, d.job[1].a, dgu, T, 2ll * I) &&
+         map_mn(h->e, d.job[1].b[0], x, T, H) && map_d(h->e, d.job[1], dgate_up, 2ll * I, H) &&
+         map_mn(h->e, d.job[2].a, dy, T, H) && map_mn(h->e, d.job[2].b[0], hbuf, T, I) && map_d(h->e, d.job[2], ddown, H, I);
     if (!ok) return WEAVE_ERR_CUDA;
     for (int i = 0; i < 3; ++i) d.job[i].b[1] = d.job[i].b[0];
-    gemm_job(d.job[0], T, H, 2ll * I, 64, gemm_width(h->e, T, H, (2 * I + 63) / 64, 256, 128, 1), false, true);
+    const double others = (gemm_tiles(2 * I, H, 256) + gemm_tiles(H, I, 256)) * gemm_tile_us((T + 63) / 64, 256);
+    gemm_job(d.job[0], T, H, 2ll * I, 64, gemm_width_among(h->e, T, H, (2 * I + 63) / 64, others), false, true);
     gemm_job(d.job[1], 2 * I, H, T, 64, 256, true, true);
     gemm_job(d.job[2], H, I, T, 64, 256, true, true);
     err = launch_gemm<kEpiStore, false>(h->e, d, 3, kGemmHalf, kBehind, stream);
@@ -657,7 +686,7 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
         if (err != cudaSuccess) return cuda_fail(h->e, err);
     }
     GemmArgs g;
-    const int wide = gemm_width(h->e, T, N, (K + 127) / 128, 256, 64, 1);
+    const int wide = gemm_width(h->e, T, N, (K + 127) / 128, 256, out_type == WEAVE_F32 ? 32 : 16, 1);
     g.direct = (size_t)N * out_size % 16 != 0;
     g.out_f32 = out_type == WEAVE_F32;
     g.out = out;
@@ -665,7 +694,7 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     g.row_scale = x_scale;
     g.col_scale = h->cfg.scale;
     if (!map_k(h->e, g.job[0].a, WEAVE_INT8, q, T, K) || !map_k(h->e, g.job[0].b[0], WEAVE_INT8, h->cfg.weight, N, K, wide / 2)) return WEAVE_ERR_CUDA;
-    if (!g.direct && !map_2d(h->e, g.job[0].d, out_type, out, T, N, 32, out_type == WEAVE_F32 ? 32 : 64)) return WEAVE_ERR_CUDA;
+    if (!g.direct && !(g.out_f32 ? map_2d(h->e, g.job[0].d, WEAVE_F32, out, T, N, 32, 32) : map_d(h->e, g.job[0], out, T, N))) return WEAVE_ERR_CUDA;
     g.job[0].b[1] = g.job[0].b[0];
     gemm_job(g.job[0], T, N, K, 128, wide, false, false);
     err = launch_gemm<kEpiScaled, true>(h->e, g, 1, wide * 64, round ? kBehind : kPlain, stream);

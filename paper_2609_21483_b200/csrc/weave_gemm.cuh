@@ -9,7 +9,7 @@
 //   kEpiScaled      D = (A B) * (row scale * column scale) in bf16 or fp32 (256)         8-bit integers, K-major
 //   kEpiScaledGated h as above from scaled g and u (128)                                 8-bit integers, K-major
 //
-// A tile is 256 rows of A (128 per CTA) by up to 256 accumulator columns (fewer where that gives idle SMs work).  A k-step
+// A tile is 256 rows of A (128 per CTA) by up to 256 accumulator columns (fewer where that fills the last wave).  A k-step
 // is 128 bytes of K (64 bf16 or 128 8-bit integers): 16 KB of A and up to 16 KB of B per CTA, 192 KB of them in flight.  Rows, columns and K that stick out over
 // the matrices are zero-filled by the tensor maps on the way in and clipped by them on the way out.
 //
@@ -144,10 +144,13 @@ struct alignas(64) GemmJob {
     CUtensorMap a;
     CUtensorMap b[2];        // [rank of the CTA in its pair]: the gated forms give gate rows to one, up rows to the other
     CUtensorMap d;           // results; kEpiGrad: h, dg, du in jobs 0, 1, 2
+    CUtensorMap d8;          // results in bf16, eight columns at a time: what a width leaves over 64
     int M, N;                // rows and columns of the result
     int ksteps;
     int a_mn, b_mn;          // kEpiStore: operand is MN-major
-    int width;               // columns of the result in a tile
+    int width;               // columns of the result in a tile: a multiple of 16 up to 256, gated of 8 up to 128; of 32 where
+                             // the result is in fp32, of 64 where B is MN-major (kEpiGrad, too): with 16 of them in a CTA
+                             // the products came out wrong, with 32 right
     int tiles_m, tiles_n, group_m;
 };
 
@@ -222,6 +225,28 @@ __device__ __forceinline__ bool gemm_tile(const GemmArgs &p, int i, int pair, in
     if (t >= n0) return false;
     gemm_tile_at(p.job[0], t, at);
     return true;
+}
+
+// A warp's 32 rows x 64 columns in bf16 on their way out: 128-byte rows, swizzled, for one tensor copy; of a narrower rest
+// of a tile eight columns lie together, for copies of their own.
+__device__ __forceinline__ uint32_t gemm_staged(uint32_t dst, int lane, int j, int there)
+{
+    return there == 64 ? dst + lane * 128 + ((j ^ (lane & 7)) << 4) : dst + j * 512 + lane * 16;
+}
+__device__ __forceinline__ void gemm_store_bf16(const GemmJob &job, uint32_t src, int lane, int col, int row0, int there, bool any_row)
+{
+    fence_proxy_async_shared();
+    __syncwarp();
+    if (lane == 0) {
+        if (any_row) {
+            if (there == 64) {
+                if (col < job.N) tma_store_2d(&job.d, src, col, row0);
+            } else {
+                for (int j = 0; j * 8 < there && col + j * 8 < job.N; ++j) tma_store_2d(&job.d8, src + j * 512, col + j * 8, row0);
+            }
+        }
+        bulk_commit();
+    }
 }
 
 template <int kEpi, bool kI8>
@@ -355,8 +380,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
 
             if constexpr (kEpi == kEpiStore || kEpi == kEpiScaled) {
 #pragma unroll 1
-                for (int c = 0; c < width / 64; ++c) {
-                    const int col = n0 + c * 64;
+                for (int c = 0; c * 64 < width; ++c) {
+                    const int col = n0 + c * 64, there = min(64, width - c * 64);
                     uint32_t v[64];
                     tmem_ld_32x64(lane_base + buf * 256 + c * 64, v);
                     tmem_ld_wait64(v);
@@ -386,7 +411,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
 #pragma unroll
                             for (int i = 0; i < 32; ++i) st_shared_u32(stage + lane * 132 + i * 4, v[half * 32 + i]);
                             __syncwarp();
-                            const int cc = col + half * 32 + lane;
+                            const int cc = half * 32 + lane < there ? col + half * 32 + lane : N;
                             const int rows = min(32, M - row0);
                             if (cc < N)
                                 for (int r = 0; r < rows; ++r) {
@@ -412,7 +437,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                                                         v[half * 32 + j * 4 + 3]));
                             fence_proxy_async_shared();
                             __syncwarp();
-                            if (lane == 0 && col + half * 32 < N) tma_store_2d(&job.d, dst, col + half * 32, row0);
+                            if (lane == 0 && half * 32 < there && col + half * 32 < N) tma_store_2d(&job.d, dst, col + half * 32, row0);
                             if (lane == 0) bulk_commit();
                         }
                     } else {
@@ -426,16 +451,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
 #pragma unroll
                             for (int q = 0; q < 4; ++q)
                                 w[q] = pack_bf16x2(__uint_as_float(v[j * 8 + q * 2]), __uint_as_float(v[j * 8 + q * 2 + 1]));
-                            st_shared_v4(dst + lane * 128 + ((j ^ (lane & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                            st_shared_v4(gemm_staged(dst, lane, j, there), make_uint4(w[0], w[1], w[2], w[3]));
                         }
-                        fence_proxy_async_shared();
-                        __syncwarp();
-                        if (lane == 0) { tma_store_2d(&job.d, dst, col, row0); bulk_commit(); }
+                        gemm_store_bf16(job, dst, lane, col, row0, there, true);
                     }
                 }
             } else if constexpr (kEpi == kEpiGated || kEpi == kEpiScaledGated) {
 #pragma unroll 1
-                for (int c = 0; c < width / 64; ++c) {
+                for (int c = 0; c * 64 < width; ++c) {
+                    const int there = min(64, width - c * 64);
                     const uint32_t dst = stage + slot * 4096;
                     slot ^= 1u;
                     if (lane == 0) bulk_wait_read<1>();
@@ -475,15 +499,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                                 w[q] = pack_bf16x2(gated(__uint_as_float(g[i]), __uint_as_float(u[i])),
                                                    gated(__uint_as_float(g[i + 1]), __uint_as_float(u[i + 1])));
                             }
-                            st_shared_v4(dst + lane * 128 + (((half * 4 + j) ^ (lane & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                            st_shared_v4(gemm_staged(dst, lane, half * 4 + j, there), make_uint4(w[0], w[1], w[2], w[3]));
                         }
                     }
-                    fence_proxy_async_shared();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (any_row && n0 + c * 64 < N) tma_store_2d(&job.d, dst, n0 + c * 64, row0);
-                        bulk_commit();
-                    }
+                    gemm_store_bf16(job, dst, lane, n0 + c * 64, row0, there, any_row);
                 }
             } else {
                 // kEpiGrad: 32 columns at a time, three results of 32 x 32 bf16 (64-byte swizzle) in rotating quarters

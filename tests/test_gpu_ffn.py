@@ -66,7 +66,7 @@ def within(got, want, bound):
 
 SHAPES = [(1, 8, 8), (2, 64, 64), (1, 2048, 768), (7, 136, 72), (16, 512, 1024), (33, 1096, 344), (64, 256, 128), (127, 264, 520),
           (128, 2048, 1408), (129, 72, 2744), (256, 256, 128), (257, 520, 136), (300, 1096, 2744), (511, 128, 64), (1023, 4096, 648),
-          (2100, 768, 1032)]
+          (2100, 768, 1032), (700, 4008, 200), (1500, 264, 4104), (4500, 136, 72)]
 
 
 @pytest.mark.parametrize("T,H,I", SHAPES)
@@ -230,7 +230,7 @@ def exact_linear(q, sx, w, sw):
     return (q.double() @ w.double().T).float() * (sx[:, None] * sw[None, :])
 
 
-INT8_SHAPES = [(1, 16, 1), (1, 7168, 2048), (2, 144, 7), (15, 4096, 264), (33, 272, 4095), (64, 128, 128), (129, 1040, 130), (256, 512, 256),
+INT8_SHAPES = [(700, 272, 9001), (1023, 400, 14336), (1500, 1040, 4120), (1, 16, 1), (1, 7168, 2048), (2, 144, 7), (15, 4096, 264), (33, 272, 4095), (64, 128, 128), (129, 1040, 130), (256, 512, 256),
                (257, 14336, 520), (1023, 2048, 1001), (2100, 400, 776)]
 
 
