@@ -68,6 +68,9 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
 int weave_ffn_status(weave_ffn_t h);
 /* Upper bound in milliseconds for any single in-kernel wait (default 4000). */
 int weave_ffn_set_timeout_ms(weave_ffn_t h, int ms);
+/* Test hook for the give-up path: thread block `cta` of a call of up to 128 tokens never arrives at a grid barrier, so the
+ * bounded waits of all expire and the call ends with WEAVE_ERR_TIMEOUT (-1 = off, the default).  Nothing faults or traps. */
+int weave_ffn_debug_withhold_arrival(weave_ffn_t h, int cta);
 int weave_ffn_last_cuda_error(weave_ffn_t h);
 /* Releases host state.  Does not touch device memory. */
 int weave_ffn_destroy(weave_ffn_t h);
@@ -76,7 +79,8 @@ int weave_ffn_destroy(weave_ffn_t h);
 
 /* Rows to 8-bit integers: scale[r] = max|x[r]| / 127 in fp32, q[r][c] = the integer nearest to x[r][c] / scale[r]
  * (decided exactly, ties to even, within +-127).  x: device, x_type WEAVE_BF16 or WEAVE_F32, [rows][cols]; q: int8
- * [rows][cols]; scale: fp32 [rows]; any cols >= 1.  A row of zeros has scale 0 and zeros; a row with an inf or a NaN
+ * [rows][cols]; scale: fp32 [rows]; cols from 1 to 16777216.
+ * A row of zeros has scale 0 and zeros; a row with an inf or a NaN
  * has scale inf or NaN and zeros, so that what is computed from it is NaN.  Serves activations (rows = tokens) and
  * weights (rows = output channels).  No handle, no workspace. */
 int weave_int8_quantize(const void *x, int x_type, int rows, int cols, void *q, float *scale, void *cuda_stream);

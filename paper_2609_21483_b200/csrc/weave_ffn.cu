@@ -22,6 +22,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
 constexpr int kMaxWidth = 65536;
 constexpr int kMaxRows = 1 << 22;
 constexpr int kMaxSms = 160;
+constexpr int kMaxCols = 1 << 24;
 
 size_t up1024(size_t n) { return (n + 1023) & ~(size_t)1023; }
 
@@ -32,6 +33,7 @@ struct Engine {
     unsigned long long timeout_ns;
     cudaStream_t last_stream;
     int last_cuda_error;
+    int withhold;              // weave_ffn_debug_withhold_arrival()
     EncodeTiledFn encode;
 };
 
@@ -88,6 +90,7 @@ int engine_create(Engine &e, void *workspace)
     e.timeout_ns = 4000ull * 1000000ull;
     e.last_stream = nullptr;
     e.last_cuda_error = 0;
+    e.withhold = -1;
     void *fn = nullptr;
     cudaDriverEntryPointQueryResult res;
     err = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &res);
@@ -241,6 +244,7 @@ cudaError_t launch_small(const Engine &e, SmallArgs &a, int T, cudaStream_t stre
 {
     a.ctl = e.ctl;
     a.timeout_ns = e.timeout_ns;
+    a.withhold = e.withhold;
     a.T = T;
     a.acc_cols = 0;
     for (int i = 0; i < a.products; ++i) {
@@ -566,6 +570,13 @@ int weave_ffn_set_timeout_ms(weave_ffn_t h, int ms)
     return WEAVE_OK;
 }
 
+int weave_ffn_debug_withhold_arrival(weave_ffn_t h, int cta)
+{
+    if (!h || cta < -1) return WEAVE_ERR_INVALID_ARG;
+    h->e.withhold = cta;
+    return WEAVE_OK;
+}
+
 int weave_ffn_last_cuda_error(weave_ffn_t h) { return h ? h->e.last_cuda_error : 0; }
 
 int weave_ffn_destroy(weave_ffn_t h)
@@ -610,7 +621,7 @@ extern "C" {
 
 int weave_int8_quantize(const void *x, int x_type, int rows, int cols, void *q, float *scale, void *cuda_stream)
 {
-    if ((x_type != WEAVE_BF16 && x_type != WEAVE_F32) || rows < 0 || cols < 1) return WEAVE_ERR_INVALID_ARG;
+    if ((x_type != WEAVE_BF16 && x_type != WEAVE_F32) || rows < 0 || cols < 1 || cols > kMaxCols) return WEAVE_ERR_INVALID_ARG;
     if (rows == 0) return WEAVE_OK;
     const size_t size = x_type == WEAVE_BF16 ? 2 : 4, n = (size_t)rows * cols;
     if (!x || !q || !scale || !aligned(x, size) || !aligned(scale, 4)) return WEAVE_ERR_INVALID_ARG;
@@ -686,8 +697,8 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
         if (err != cudaSuccess) return cuda_fail(h->e, err);
     }
     GemmArgs g;
-    const int wide = gemm_width(h->e, T, N, (K + 127) / 128, 256, out_type == WEAVE_F32 ? 32 : 16, 1);
     g.direct = (size_t)N * out_size % 16 != 0;
+    const int wide = gemm_width(h->e, T, N, (K + 127) / 128, 256, out_type == WEAVE_F32 && !g.direct ? 32 : 16, 1);
     g.out_f32 = out_type == WEAVE_F32;
     g.out = out;
     g.ld_out = N;

@@ -235,6 +235,7 @@ struct alignas(64) SmallArgs {
     FfnCtl *ctl;
     unsigned long long timeout_ns;
     int products, T;
+    int withhold;            // test hook: this CTA never arrives at a grid barrier (-1: none)
     int acc_cols, tmem_cols;
 };
 
@@ -257,13 +258,14 @@ __device__ __forceinline__ unsigned long long small_barrier_target(const unsigne
     const unsigned long long g = gridDim.x;
     return (ld_acquire_u64(counter) / g + 1) * g;
 }
-__device__ __forceinline__ bool small_grid_barrier(unsigned long long *counter, unsigned long long target, bool ok, const WaitCtx &wc, int where)
+__device__ __forceinline__ bool small_grid_barrier(unsigned long long *counter, unsigned long long target, bool ok, bool withheld, const WaitCtx &wc,
+                                                   int where)
 {
     __threadfence();
     fence_proxy_async_global();          // ordinary stores here, tensor-map loads there
     ok = named_barrier_and<1, 256>(ok);
     if (ok && threadIdx.x == 128) {
-        red_release_add_u64(counter, 1ull);
+        if (!withheld) red_release_add_u64(counter, 1ull);
         unsigned long long t0 = 0;
         unsigned it = 0;
         while (ld_acquire_u64(counter) < target) {
@@ -419,6 +421,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
         const int quarter = warp & 3, group = (warp - 4) >> 2, tid = threadIdx.x - 128 - group * 128;
         const int acc_row = quarter * 32 + lane;
         uint32_t *const red = reinterpret_cast<uint32_t *>(behind + group * kSmallRed);
+        const bool withheld = (int)blockIdx.x == a.withhold;
         unsigned long long target[3] = {0, 0, 0};
         if (threadIdx.x == 128)
 #pragma unroll
@@ -429,7 +432,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
             const SmallProduct &p = a.p[i];
             const SmallShape s = p.s;
             const bool gate = p.gated, out_f32 = p.out_f32;
-            if (i > 0) ok = small_grid_barrier(&a.ctl->barrier[0], target[0], ok, wc, 26);
+            if (i > 0) ok = small_grid_barrier(&a.ctl->barrier[0], target[0], ok, withheld, wc, 26);
             if constexpr (kI8) {
                 if (ok && p.round_src) {
                     if (p.round_f32) small_round_rows(static_cast<const float *>(p.round_src), p, a.T, bars.row_max);
@@ -438,7 +441,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
                         fence_proxy_async_global();
                         named_barrier_sync<1, 256>();
                     } else {
-                        ok = small_grid_barrier(&a.ctl->barrier[1 + i], i == 0 ? target[1] : target[2], ok, wc, 27);
+                        ok = small_grid_barrier(&a.ctl->barrier[1 + i], i == 0 ? target[1] : target[2], ok, withheld, wc, 27);
                     }
                 }
             }

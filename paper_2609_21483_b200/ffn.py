@@ -14,7 +14,7 @@ BF16, F32, INT8 = 0, 1, 2
 
 EXPORTS = [
     "weave_ffn_workspace_bytes", "weave_ffn_create", "weave_ffn_forward", "weave_ffn_backward", "weave_ffn_status",
-    "weave_ffn_set_timeout_ms", "weave_ffn_last_cuda_error", "weave_ffn_destroy",
+    "weave_ffn_set_timeout_ms", "weave_ffn_debug_withhold_arrival", "weave_ffn_last_cuda_error", "weave_ffn_destroy",
     "weave_int8_quantize", "weave_int8_linear_workspace_bytes", "weave_int8_linear_create",
     "weave_int8_linear_forward", "weave_int8_linear_status", "weave_int8_linear_set_timeout_ms",
     "weave_int8_linear_last_cuda_error", "weave_int8_linear_destroy",
@@ -53,6 +53,7 @@ def load():
                        ("weave_ffn_forward", [vp, vp, vp, ci, vp]),
                        ("weave_ffn_backward", [vp, vp, vp, vp, vp, vp, ci, vp]),
                        ("weave_ffn_status", [vp]), ("weave_ffn_set_timeout_ms", [vp, ci]),
+                       ("weave_ffn_debug_withhold_arrival", [vp, ci]),
                        ("weave_ffn_last_cuda_error", [vp]), ("weave_ffn_destroy", [vp]),
                        ("weave_int8_quantize", [vp, ci, ci, ci, vp, vp, vp]),
                        ("weave_int8_linear_create", [ctypes.POINTER(_Int8LinearConfig), vpp]),
@@ -201,6 +202,9 @@ class GatedFFN(_Handle):
         self._call(self._lib.weave_ffn_forward, x.data_ptr(), out.data_ptr(), T, stream=stream)
         return out
 
+    def debug_withhold_arrival(self, cta: int):
+        _check(self._lib.weave_ffn_debug_withhold_arrival(self._h, cta), "weave_ffn_debug_withhold_arrival")
+
     def backward(self, x, dy, dx=None, dgate_up=None, ddown=None, stream: Optional[int] = None):
         """(dx [T, H], dgate_up [2I, H], ddown [H, I]) in bf16 for the gradient dy of forward(x); all overwritten."""
         torch = self._torch
@@ -237,6 +241,7 @@ class Int8FFN(_Handle):
 
     _rows = GatedFFN._rows
     forward = GatedFFN.forward
+    debug_withhold_arrival = GatedFFN.debug_withhold_arrival
 
 
 class Int8Linear(_Handle):

@@ -87,6 +87,7 @@ def test_calls_without_a_handle(lib):
     assert lib.weave_ffn_forward(None, None, None, 1, None) == INVALID
     assert lib.weave_ffn_backward(None, None, None, None, None, None, 1, None) == INVALID
     assert lib.weave_ffn_status(None) == INVALID and lib.weave_ffn_set_timeout_ms(None, 5) == INVALID
+    assert lib.weave_ffn_debug_withhold_arrival(None, 0) == INVALID
     assert lib.weave_ffn_destroy(None) == 0 and lib.weave_int8_linear_destroy(None) == 0
     assert lib.weave_int8_linear_forward(None, None, 0, None, None, 0, 1, None) == INVALID
     assert lib.weave_int8_linear_status(None) == INVALID
@@ -97,6 +98,7 @@ def test_quantize_refuses(lib):
     a, q, s = 0x10000, 0x20000, 0x30000
     assert f(a, 2, 4, 4, q, s, None) == INVALID          # int8 input
     assert f(a, 0, -1, 4, q, s, None) == INVALID and f(a, 0, 4, 0, q, s, None) == INVALID
+    assert f(a, 0, 1, (1 << 24) + 1, q, s, None) == INVALID
     assert f(None, 0, 4, 4, q, s, None) == INVALID and f(a, 0, 4, 4, None, s, None) == INVALID and f(a, 0, 4, 4, q, None, None) == INVALID
     assert f(a + 1, 0, 4, 4, q, s, None) == INVALID and f(a + 2, 1, 4, 4, q, s, None) == INVALID and f(a, 0, 4, 4, q, s + 2, None) == INVALID
     assert f(a, 0, 4, 4, a + 8, s, None) == INVALID      # q inside x

@@ -412,3 +412,106 @@ def test_refusals_on_the_device():
         pk.GatedFFN(torch.zeros(24, 20, dtype=torch.bfloat16, device="cuda"), torch.zeros(20, 12, dtype=torch.bfloat16, device="cuda"))
     ffn.check()
     ffn.close()
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_a_wait_that_gives_up_ends_the_call(int8):
+    """One thread block never arrives: every wait behind that barrier expires, the call ends with a status, and the handle
+    works again."""
+    T, H, I = 5, 272, 400
+    x, gate_up, down, _ = block(T, H, I, seed=6)
+    if int8:
+        ffn = pk.Int8FFN(*pk.quantize_rows(gate_up), *pk.quantize_rows(down), max_tokens=T)
+    else:
+        ffn = pk.GatedFFN(gate_up, down, max_tokens=T)
+    want = ffn.forward(x)
+    ffn.check()
+    ffn.set_timeout_ms(20)
+    ffn.debug_withhold_arrival(3)
+    ffn.forward(x)
+    assert ffn.status() == pk.ERR_TIMEOUT
+    ffn.debug_withhold_arrival(-1)
+    ffn.set_timeout_ms(4000)
+    for _ in range(3):
+        assert torch.equal(ffn.forward(x), want)
+    ffn.check()
+    with pytest.raises(pk.WeaveError):
+        ffn.debug_withhold_arrival(-2)
+    ffn.close()
+
+
+def test_two_handles_on_two_streams():
+    """Small and large batches of two handles side by side: what each computes does not change."""
+    H, I = 528, 400
+    x, gate_up, down, dy = block(300, H, I, seed=31)
+    (gq, gs), (dq, ds) = pk.quantize_rows(gate_up), pk.quantize_rows(down)
+    a, b = pk.GatedFFN(gate_up, down, max_tokens=300, backward=True), pk.Int8FFN(gq, gs, dq, ds, max_tokens=300)
+    sizes = (1, 40, 300)
+    want = {(k, n): m.forward(x[:n]) for k, m in (("a", a), ("b", b)) for n in sizes}
+    grads = a.backward(x, dy)
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for _ in range(40):
+        for n in sizes:
+            for (k, m), s in zip((("a", a), ("b", b)), streams):
+                with torch.cuda.stream(s):
+                    got.append((k, n, m.forward(x[:n])))
+        with torch.cuda.stream(streams[0]):
+            g = a.backward(x, dy)
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
+    assert all(torch.equal(want[k, n], y) for k, n, y in got)
+    assert all(torch.equal(p, q) for p, q in zip(g, grads))
+    a.close()
+    b.close()
+
+
+def test_two_graphs_of_one_handle_in_turn():
+    """Both use the handle's workspace; replayed in the order of a stream they do not disturb one another."""
+    H, I = 272, 400
+    x, gate_up, down, _ = block(200, H, I, seed=41)
+    ffn = pk.GatedFFN(gate_up, down, max_tokens=200)
+    outs = [torch.empty(n, H, dtype=torch.bfloat16, device="cuda") for n in (20, 200)]
+    want = [ffn.forward(x[:n]) for n in (20, 200)]
+    graphs = []
+    for o in outs:
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            ffn.forward(x[:o.shape[0]], out=o)
+        graphs.append(g)
+    for _ in range(20):
+        for g, o in zip(graphs, outs):
+            o.zero_()
+            g.replay()
+        eager = ffn.forward(x[:20])
+    torch.cuda.synchronize()
+    ffn.check()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want)) and torch.equal(eager, want[0])
+    ffn.close()
+
+
+@pytest.mark.parametrize("T", [1, 8, 9, 16, 24, 48, 100, 128])
+def test_small_batches_of_every_plan(T):
+    """Every number of K blocks per step, whole and broken last steps, one and several tiles per thread block."""
+    for H, I in ((64, 64), (128, 24), (448, 136), (1088, 320), (192, 20000), (2968, 9600), (2048, 4736)):
+        x, gate_up, down, _ = block(T, H, I, seed=T + H)
+        ffn = pk.GatedFFN(gate_up, down, max_tokens=T)
+        within(ffn.forward(x), *forward_and_bound(x, gate_up, down))
+        ffn.check()
+        ffn.close()
+
+
+def test_a_row_does_not_depend_on_the_batch():
+    """The same token alone, in a small batch and in a large one: 8-bit products are the same bits, bf16 ones within a rounding."""
+    H, I = 1024, 1408
+    x, gate_up, down, _ = block(300, H, I, seed=51)
+    (gq, gs), (dq, ds) = pk.quantize_rows(gate_up), pk.quantize_rows(down)
+    lin = pk.Int8Linear(gq, gs, max_tokens=300)
+    all_rows = lin.forward(x, out_dtype=torch.float32)
+    for n in (1, 2, 3, 17, 128, 129):
+        assert torch.equal(lin.forward(x[:n], out_dtype=torch.float32), all_rows[:n])
+    lin.check()
+    lin.close()
