@@ -183,6 +183,20 @@ cudaError_t launch(void (*kernel)(Params...), int grid, int block, size_t smem, 
     return cudaLaunchKernelEx(&lc, kernel, args...);
 }
 
+// Which kernel takes a call of up to kSmallMaxT tokens: the one whose modelled time is shorter, the products' cost and what
+// else was measured of each.  (us, one launch against pairs of SMs: bf16 2048 x 768: 10.1 / 16.3 with 16 tokens, 16.4 / 16.8
+// with 64, 18.6 / 16.2 with 96; 4096 x 14336: 76 / 92 with 64, 82 / 93 with 96; 8 bits 2048 x 1408: 16.6 / 18.3 with 16,
+// 21.6 / 18.4 with 64; 4096 x 14336: 52 / 58 with 64, 61 / 59 with 128.)
+bool small_wins(int T, int products, bool rounds, double small_us, double pairs_us)
+{
+    const double small_rest = 1.0 + products * (rounds ? 6.0 : 3.0) + products * 0.033 * T, pairs_rest = products * (rounds ? 6.5 : 4.0);
+    return small_rest + small_us <= pairs_rest + pairs_us;
+}
+double small_us(const Engine &e, int n, bool gated, long long K, int block, int T)
+{
+    return small_cost(small_plan(n, gated, K, block, T, e.n_sm), K, block, T);
+}
+
 // The first product of a, or the next one: its plan and its tensor maps.  x: what the product reads, [copies][T][K].
 bool small_product(const Engine &e, SmallArgs &a, int type, const void *w, const void *x, int n, bool gated, int K, int T, const float *row_scale,
                    const float *col_scale, void *out, bool out_f32, int copies)
@@ -265,17 +279,14 @@ double gemm_tile_us(int ksteps, int accumulator_columns)
     return ksteps * step > epilogue ? ksteps * step : epilogue;
 }
 long long gemm_tiles(int M, int N, int width) { return (long long)((M + 255) / 256) * ((N + width - 1) / width); }
-int gemm_width(const Engine &e, int M, int N, int ksteps, int widest, int unit, int columns)
+struct GemmWidth { int width; double us; };
+GemmWidth gemm_width(const Engine &e, int M, int N, int ksteps, int widest, int unit, int columns)
 {
-    int best = widest;
-    double best_cost = 1e30;
+    GemmWidth best = {widest, 1e30};
     for (int w = widest; w * columns >= 64 && w > 0; w -= unit) {
         const long long pairs = e.n_sm / 2, waves = (gemm_tiles(M, N, w) + pairs - 1) / pairs;
-        const double cost = waves * gemm_tile_us(ksteps, w * columns) + 0.008 * w * columns;
-        if (cost < best_cost) {
-            best_cost = cost;
-            best = w;
-        }
+        const double us = waves * gemm_tile_us(ksteps, w * columns) + 0.008 * w * columns;
+        if (us < best.us) best = {w, us};
     }
     return best;
 }
@@ -463,7 +474,9 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     const int type = i8 ? WEAVE_INT8 : WEAVE_BF16;
     const void *left = i8 ? static_cast<const void *>(xq) : x, *mid = i8 ? static_cast<const void *>(hq) : hbuf;
     cudaError_t err = cudaSuccess;
-    if (T <= kSmallMaxT) {
+    const int step = i8 ? 128 : 64;
+    const GemmWidth up_w = gemm_width(h->e, T, I, (H + step - 1) / step, 128, 8, 2), down_w = gemm_width(h->e, T, H, (I + step - 1) / step, 256, 16, 1);
+    if (T <= kSmallMaxT && small_wins(T, 2, i8, small_us(h->e, I, true, H, step, T) + small_us(h->e, H, false, I, step, T), up_w.us + down_w.us)) {
         SmallArgs a;
         a.products = 0;
         if (!small_product(h->e, a, type, h->cfg.gate_up, left, I, true, H, T, xs, h->cfg.gate_up_scale, hbuf, false,
@@ -477,10 +490,8 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     }
     // the wide products: gate and up with the activation, then down
     GemmArgs g, d;
-    const int step = i8 ? 128 : 64;
-    const size_t wsize1 = i8 ? 1 : 2;
-    const int wide = gemm_width(h->e, T, I, (H + step - 1) / step, 128, 8, 2), wide_d = gemm_width(h->e, T, H, (I + step - 1) / step, 256, 16, 1);
-    const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * wsize1;
+    const int wide = up_w.width, wide_d = down_w.width;
+    const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * wsize;
     if (!map_k(h->e, g.job[0].a, type, left, T, H) || !map_k(h->e, g.job[0].b[0], type, h->cfg.gate_up, I, H, wide) ||
         !map_k(h->e, g.job[0].b[1], type, up, I, H, wide) || !map_d(h->e, g.job[0], hbuf, T, I) ||
         !map_k(h->e, d.job[0].a, type, mid, T, I) || !map_k(h->e, d.job[0].b[0], type, h->cfg.down, H, I, wide_d / 2) ||
@@ -527,7 +538,7 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     uint8_t *hbuf = h->ws + h->L.h, *dgu = h->ws + h->L.dgu;
     // h and [dg du] from x and dy
     GemmArgs g;
-    const int wide = gemm_width(h->e, T, I, (H + 63) / 64 * 3 / 2, 128, 64, 2);
+    const int wide = gemm_width(h->e, T, I, (H + 63) / 64 * 3 / 2, 128, 64, 2).width;
     const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * 2;
     bool ok = map_k(h->e, g.job[0].a, WEAVE_BF16, dy, T, H) && map_mn(h->e, g.job[0].b[0], h->cfg.down, H, I) &&
               map_k(h->e, g.job[1].a, WEAVE_BF16, x, T, H) && map_k(h->e, g.job[1].b[0], WEAVE_BF16, h->cfg.gate_up, I, H, wide) &&
@@ -682,7 +693,9 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     const bool round = x_type != WEAVE_INT8;
     const void *q = round ? xq : x;
     if (round) x_scale = xs;
-    if (T <= kSmallMaxT) {
+    const bool direct = (size_t)N * out_size % 16 != 0;
+    const GemmWidth w = gemm_width(h->e, T, N, (K + 127) / 128, 256, out_type == WEAVE_F32 && !direct ? 32 : 16, 1);
+    if (T <= kSmallMaxT && small_wins(T, 1, round, small_us(h->e, N, false, K, 128, T), w.us)) {
         SmallArgs a;
         a.products = 0;
         if (!small_product(h->e, a, WEAVE_INT8, h->cfg.weight, q, N, false, K, T, x_scale, h->cfg.scale, out, out_type == WEAVE_F32,
@@ -697,8 +710,8 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
         if (err != cudaSuccess) return cuda_fail(h->e, err);
     }
     GemmArgs g;
-    g.direct = (size_t)N * out_size % 16 != 0;
-    const int wide = gemm_width(h->e, T, N, (K + 127) / 128, 256, out_type == WEAVE_F32 && !g.direct ? 32 : 16, 1);
+    const int wide = w.width;
+    g.direct = direct;
     g.out_f32 = out_type == WEAVE_F32;
     g.out = out;
     g.ld_out = N;
