@@ -414,6 +414,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                             const int cc = half * 32 + lane < there ? col + half * 32 + lane : N;
                             const int rows = min(32, M - row0);
                             if (cc < N)
+#pragma unroll 8
                                 for (int r = 0; r < rows; ++r) {
                                     const float y = ld_shared_f32(stage + r * 132 + lane * 4);
                                     const long long at = (long long)(row0 + r) * p.ld_out + cc;
