@@ -40,6 +40,7 @@ struct Engine {
 int cuda_fail(Engine &e, cudaError_t err)
 {
     e.last_cuda_error = (int)err;
+    (void)cudaGetLastError();       // reported here: not once more to whoever asks the runtime next
     return WEAVE_ERR_CUDA;
 }
 
@@ -132,12 +133,13 @@ bool on_its_device(const Engine &e)
     return cudaGetDevice(&dev) == cudaSuccess && dev == e.device;
 }
 
-// [rows][cols] row-major, box of box_cols x box_rows
-bool map_2d(const Engine &e, CUtensorMap &m, int type, const void *p, long long rows, long long cols, int box_rows, int box_cols)
+// [rows][cols] row-major, rows `pitch` elements apart (0: cols), box of box_cols x box_rows
+bool map_2d(const Engine &e, CUtensorMap &m, int type, const void *p, long long rows, long long cols, int box_rows, int box_cols,
+            long long pitch = 0)
 {
     const int size = type == WEAVE_BF16 ? 2 : type == WEAVE_F32 ? 4 : 1;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)cols * size};
+    const cuuint64_t strides[1] = {(cuuint64_t)(pitch ? pitch : cols) * size};
     const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
     const cuuint32_t ones[2] = {1, 1};
     const CUtensorMapDataType dt = type == WEAVE_BF16  ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
@@ -150,14 +152,14 @@ bool map_2d(const Engine &e, CUtensorMap &m, int type, const void *p, long long 
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // operand whose K runs along the rows' elements: some rows x 128 bytes
-bool map_k(const Engine &e, CUtensorMap &m, int type, const void *p, long long rows, long long cols, int box_rows = 128)
+bool map_k(const Engine &e, CUtensorMap &m, int type, const void *p, long long rows, long long cols, int box_rows = 128, long long pitch = 0)
 {
-    return map_2d(e, m, type, p, rows, cols, box_rows, type == WEAVE_INT8 ? 128 : 64);
+    return map_2d(e, m, type, p, rows, cols, box_rows, type == WEAVE_INT8 ? 128 : 64, pitch);
 }
 // operand whose K runs across the rows (bf16): 64 elements x 64 rows
-bool map_mn(const Engine &e, CUtensorMap &m, const void *p, long long rows, long long cols)
+bool map_mn(const Engine &e, CUtensorMap &m, const void *p, long long rows, long long cols, long long pitch = 0)
 {
-    return map_2d(e, m, WEAVE_BF16, p, rows, cols, 64, 64);
+    return map_2d(e, m, WEAVE_BF16, p, rows, cols, 64, 64, pitch);
 }
 
 // kBehind: launched while the launch before it in the stream, one of the same call, still runs (see pdl_wait())
@@ -291,7 +293,8 @@ GemmWidth gemm_width(const Engine &e, int M, int N, int ksteps, int widest, int 
     return best;
 }
 // ... of the long product in a launch with others, which fill the pairs that it leaves: the longer of its own waves and
-// of all work spread evenly.  (dx of T = 777, 1096 x 2744, all three products, us with 256, 128, 64 columns: 40, 32, 52.)
+// of all work spread evenly.  (Whole gradient, us with 256, 192, 128, 64 columns of dx in a tile: T = 257, 2048 x 1408: 35.5,
+// 32.1, 30.7, 34.6; T = 777, 1096 x 2744: 66.5, 66.1, 67.0, 74.4.)
 int gemm_width_among(const Engine &e, int M, int N, int ksteps, double others_us)
 {
     int best = 256;
@@ -322,9 +325,9 @@ void gemm_job(GemmJob &j, int M, int N, long long K, int step, int width, bool a
 }
 
 // a result in bf16
-bool map_d(const Engine &e, GemmJob &j, const void *p, long long rows, long long cols)
+bool map_d(const Engine &e, GemmJob &j, const void *p, long long rows, long long cols, long long pitch = 0)
 {
-    return map_2d(e, j.d, WEAVE_BF16, p, rows, cols, 32, 64) && map_2d(e, j.d8, WEAVE_BF16, p, rows, cols, 32, 8);
+    return map_2d(e, j.d, WEAVE_BF16, p, rows, cols, 32, 64, pitch) && map_2d(e, j.d8, WEAVE_BF16, p, rows, cols, 32, 8, pitch);
 }
 
 // jobs: of a.job; b_bytes: B's bytes of a k-step in one CTA, at most
@@ -343,9 +346,7 @@ cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int jobs, int b_bytes, Lau
     a.extra = 0;
     if (kEpi == kEpiStore) {
         for (int i = jobs; i < 3; ++i) a.job[i].tiles_m = a.job[i].tiles_n = 0;
-        if (jobs > 1) {
-            a.extra = (int)(gemm_tile_us(a.job[0].ksteps, a.job[0].width) / gemm_tile_us(a.job[1].ksteps, a.job[1].width) + 0.5);
-        }
+        if (jobs > 1) a.extra = (int)(gemm_tile_us(a.job[0].ksteps, a.job[0].width) / gemm_tile_us(a.job[1].ksteps, a.job[1].width) + 0.5);
     }
     return launch(weave_gemm_kernel<kEpi, kI8>, used * 2, kGemmThreads, kGemmSmemBytes, kind, stream, a);
 }
@@ -387,6 +388,9 @@ bool ffn_shape_ok(const weave_ffn_config *c)
     return c->hidden > 0 && c->ffn > 0 && c->hidden % unit == 0 && c->ffn % unit == 0 && c->hidden <= kMaxWidth && c->ffn <= kMaxWidth &&
            c->max_tokens > 0 && c->max_tokens <= kMaxRows && (c->backward == 0 || (c->backward == 1 && c->weight_type == WEAVE_BF16));
 }
+// Rows of h and of [dg du] start on 128-byte lines: a copy's 128 bytes that straddle two take twice the requests (the
+// gradient of T = 777, 1096 x 2744: 67 -> 64 us; were x and the weights aligned, too, 55).
+long long line_pitch(long long cols) { return (cols + 63) / 64 * 64; }
 FfnLayout ffn_layout(const weave_ffn_config *c)
 {
     FfnLayout L;
@@ -395,10 +399,10 @@ FfnLayout ffn_layout(const weave_ffn_config *c)
     size_t at = up1024(sizeof(FfnCtl));
     L.control = at;
     L.h = at;
-    at += up1024(T * I * 2);
+    at += up1024(T * (size_t)line_pitch(c->ffn) * 2);
     if (c->backward) {
         L.dgu = at;
-        at += up1024(T * 2 * I * 2);
+        at += up1024(T * (size_t)line_pitch(2ll * c->ffn) * 2);
     }
     if (c->weight_type == WEAVE_INT8) {
         L.xq = at;
@@ -493,8 +497,8 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     const int wide = up_w.width, wide_d = down_w.width;
     const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * wsize;
     if (!map_k(h->e, g.job[0].a, type, left, T, H) || !map_k(h->e, g.job[0].b[0], type, h->cfg.gate_up, I, H, wide) ||
-        !map_k(h->e, g.job[0].b[1], type, up, I, H, wide) || !map_d(h->e, g.job[0], hbuf, T, I) ||
-        !map_k(h->e, d.job[0].a, type, mid, T, I) || !map_k(h->e, d.job[0].b[0], type, h->cfg.down, H, I, wide_d / 2) ||
+        !map_k(h->e, g.job[0].b[1], type, up, I, H, wide) || !map_d(h->e, g.job[0], hbuf, T, I, i8 ? 0 : line_pitch(I)) ||
+        !map_k(h->e, d.job[0].a, type, mid, T, I, 128, i8 ? 0 : line_pitch(I)) || !map_k(h->e, d.job[0].b[0], type, h->cfg.down, H, I, wide_d / 2) ||
         !map_d(h->e, d.job[0], out, T, H))
         return WEAVE_ERR_CUDA;
     gemm_job(g.job[0], T, I, H, step, wide, false, false);
@@ -542,9 +546,9 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * 2;
     bool ok = map_k(h->e, g.job[0].a, WEAVE_BF16, dy, T, H) && map_mn(h->e, g.job[0].b[0], h->cfg.down, H, I) &&
               map_k(h->e, g.job[1].a, WEAVE_BF16, x, T, H) && map_k(h->e, g.job[1].b[0], WEAVE_BF16, h->cfg.gate_up, I, H, wide) &&
-              map_k(h->e, g.job[1].b[1], WEAVE_BF16, up, I, H, wide) && map_2d(h->e, g.job[0].d, WEAVE_BF16, hbuf, T, I, 32, 32);
+              map_k(h->e, g.job[1].b[1], WEAVE_BF16, up, I, H, wide) && map_2d(h->e, g.job[0].d, WEAVE_BF16, hbuf, T, I, 32, 32, line_pitch(I));
     // d(gate) and d(up) lie side by side in rows of 2I; their maps end where their half ends
-    const cuuint64_t dims[2] = {(cuuint64_t)I, (cuuint64_t)T}, strides[1] = {(cuuint64_t)I * 4};
+    const cuuint64_t dims[2] = {(cuuint64_t)I, (cuuint64_t)T}, strides[1] = {(cuuint64_t)line_pitch(2ll * I) * 2};
     const cuuint32_t box[2] = {32, 32}, ones[2] = {1, 1};
     for (int half = 0; half < 2 && ok; ++half)
         ok = h->e.encode(&g.job[1 + half].d, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dgu + (size_t)half * I * 2, dims, strides, box, ones,
@@ -558,10 +562,10 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     if (err != cudaSuccess) return cuda_fail(h->e, err);
     // dx = [dg du] W_gu, dW_gu = [dg du]^T x, dW_d = dy^T h: one launch, so that their last waves fill one another
     GemmArgs d;
-    ok = map_k(h->e, d.job[0].a, WEAVE_BF16, dgu, T, 2ll * I) && map_mn(h->e, d.job[0].b[0], h->cfg.gate_up, 2ll * I, H) &&
-         map_d(h->e, d.job[0], dx, T, H) && map_mn(h->e, d.job[1].a, dgu, T, 2ll * I) &&
+    ok = map_k(h->e, d.job[0].a, WEAVE_BF16, dgu, T, 2ll * I, 128, line_pitch(2ll * I)) && map_mn(h->e, d.job[0].b[0], h->cfg.gate_up, 2ll * I, H) &&
+         map_d(h->e, d.job[0], dx, T, H) && map_mn(h->e, d.job[1].a, dgu, T, 2ll * I, line_pitch(2ll * I)) &&
          map_mn(h->e, d.job[1].b[0], x, T, H) && map_d(h->e, d.job[1], dgate_up, 2ll * I, H) &&
-         map_mn(h->e, d.job[2].a, dy, T, H) && map_mn(h->e, d.job[2].b[0], hbuf, T, I) && map_d(h->e, d.job[2], ddown, H, I);
+         map_mn(h->e, d.job[2].a, dy, T, H) && map_mn(h->e, d.job[2].b[0], hbuf, T, I, line_pitch(I)) && map_d(h->e, d.job[2], ddown, H, I);
     if (!ok) return WEAVE_ERR_CUDA;
     for (int i = 0; i < 3; ++i) d.job[i].b[1] = d.job[i].b[0];
     const double others = (gemm_tiles(2 * I, H, 256) + gemm_tiles(H, I, 256)) * gemm_tile_us((T + 63) / 64, 256);
@@ -638,9 +642,10 @@ int weave_int8_quantize(const void *x, int x_type, int rows, int cols, void *q, 
     if (!x || !q || !scale || !aligned(x, size) || !aligned(scale, 4)) return WEAVE_ERR_INVALID_ARG;
     const Range outs[2] = {{q, n}, {scale, (size_t)rows * 4}}, ins[1] = {{x, n * size}};
     if (!outputs_clear(outs, 2, ins, 1)) return WEAVE_ERR_INVALID_ARG;
-    return launch_quant(x, x_type, rows, cols, static_cast<int8_t *>(q), scale, kPlain, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess
-               ? WEAVE_OK
-               : WEAVE_ERR_CUDA;
+    if (launch_quant(x, x_type, rows, cols, static_cast<int8_t *>(q), scale, kPlain, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess)
+        return WEAVE_OK;
+    (void)cudaGetLastError();
+    return WEAVE_ERR_CUDA;
 }
 
 size_t weave_int8_linear_workspace_bytes(const weave_int8_linear_config *cfg)
