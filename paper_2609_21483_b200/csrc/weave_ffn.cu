@@ -146,9 +146,7 @@ bool map_2d(const Engine &e, CUtensorMap &m, int type, const void *p, long long 
                                    : type == WEAVE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                                        : CU_TENSOR_MAP_DATA_TYPE_UINT8;
     return e.encode(&m, dt, 2, const_cast<void *>(p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    box_cols * size == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
-                    : box_cols * size == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
-                                            : CU_TENSOR_MAP_SWIZZLE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // operand whose K runs along the rows' elements: some rows x 128 bytes
@@ -311,7 +309,14 @@ int gemm_width_among(const Engine &e, int M, int N, int ksteps, double others_us
     return best;
 }
 
-void gemm_job(GemmJob &j, int M, int N, long long K, int step, int width, bool a_mn, bool b_mn)
+// Rows of A per CTA where A is K-major: those of the matrix spread evenly over its tiles.
+int gemm_rows(int M)
+{
+    const int tiles = (M + 255) / 256;
+    return (((M + 2 * tiles - 1) / (2 * tiles)) + 7) & ~7;
+}
+
+void gemm_job(GemmJob &j, int M, int N, long long K, int step, int width, bool a_mn, bool b_mn, void *out, long long ld)
 {
     j.M = M;
     j.N = N;
@@ -319,15 +324,12 @@ void gemm_job(GemmJob &j, int M, int N, long long K, int step, int width, bool a
     j.a_mn = a_mn;
     j.b_mn = b_mn;
     j.width = width;
-    j.tiles_m = (M + 255) / 256;
+    j.out = out;
+    j.ld = ld;
+    j.rows = a_mn ? 128 : gemm_rows(M);
+    j.tiles_m = (M + 2 * j.rows - 1) / (2 * j.rows);
     j.tiles_n = (N + width - 1) / width;
     j.group_m = 8;
-}
-
-// a result in bf16
-bool map_d(const Engine &e, GemmJob &j, const void *p, long long rows, long long cols, long long pitch = 0)
-{
-    return map_2d(e, j.d, WEAVE_BF16, p, rows, cols, 32, 64, pitch) && map_2d(e, j.d8, WEAVE_BF16, p, rows, cols, 32, 8, pitch);
 }
 
 // jobs: of a.job; b_bytes: B's bytes of a k-step in one CTA, at most
@@ -336,7 +338,9 @@ cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int jobs, int b_bytes, Lau
 {
     a.ctl = e.ctl;
     a.timeout_ns = e.timeout_ns;
-    a.stage_bytes = kGemmHalf + b_bytes;
+    a.a_bytes = 0;
+    for (int i = 0; i < jobs; ++i) a.a_bytes = a.job[i].rows * 128 > a.a_bytes ? a.job[i].rows * 128 : a.a_bytes;
+    a.stage_bytes = a.a_bytes + b_bytes;
     a.stages = kGemmRing / a.stage_bytes;
     if (a.stages > kGemmMaxStages) a.stages = kGemmMaxStages;
     const long long pairs = e.n_sm / 2;
@@ -496,13 +500,14 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     GemmArgs g, d;
     const int wide = up_w.width, wide_d = down_w.width;
     const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * wsize;
-    if (!map_k(h->e, g.job[0].a, type, left, T, H) || !map_k(h->e, g.job[0].b[0], type, h->cfg.gate_up, I, H, wide) ||
-        !map_k(h->e, g.job[0].b[1], type, up, I, H, wide) || !map_d(h->e, g.job[0], hbuf, T, I, i8 ? 0 : line_pitch(I)) ||
-        !map_k(h->e, d.job[0].a, type, mid, T, I, 128, i8 ? 0 : line_pitch(I)) || !map_k(h->e, d.job[0].b[0], type, h->cfg.down, H, I, wide_d / 2) ||
-        !map_d(h->e, d.job[0], out, T, H))
+    const long long pitch = i8 ? I : line_pitch(I);
+    const int rows_a = gemm_rows(T);
+    if (!map_k(h->e, g.job[0].a, type, left, T, H, rows_a) || !map_k(h->e, g.job[0].b[0], type, h->cfg.gate_up, I, H, wide) ||
+        !map_k(h->e, g.job[0].b[1], type, up, I, H, wide) || !map_k(h->e, d.job[0].a, type, mid, T, I, rows_a, pitch) ||
+        !map_k(h->e, d.job[0].b[0], type, h->cfg.down, H, I, wide_d / 2))
         return WEAVE_ERR_CUDA;
-    gemm_job(g.job[0], T, I, H, step, wide, false, false);
-    gemm_job(d.job[0], T, H, I, step, wide_d, false, false);
+    gemm_job(g.job[0], T, I, H, step, wide, false, false, hbuf, pitch);
+    gemm_job(d.job[0], T, H, I, step, wide_d, false, false, out, H);
     g.row_scale = xs;
     g.col_scale = h->cfg.gate_up_scale;
     d.job[0].b[1] = d.job[0].b[0];
@@ -544,34 +549,30 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     GemmArgs g;
     const int wide = gemm_width(h->e, T, I, (H + 63) / 64 * 3 / 2, 128, 64, 2).width;
     const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * 2;
-    bool ok = map_k(h->e, g.job[0].a, WEAVE_BF16, dy, T, H) && map_mn(h->e, g.job[0].b[0], h->cfg.down, H, I) &&
-              map_k(h->e, g.job[1].a, WEAVE_BF16, x, T, H) && map_k(h->e, g.job[1].b[0], WEAVE_BF16, h->cfg.gate_up, I, H, wide) &&
-              map_k(h->e, g.job[1].b[1], WEAVE_BF16, up, I, H, wide) && map_2d(h->e, g.job[0].d, WEAVE_BF16, hbuf, T, I, 32, 32, line_pitch(I));
-    // d(gate) and d(up) lie side by side in rows of 2I; their maps end where their half ends
-    const cuuint64_t dims[2] = {(cuuint64_t)I, (cuuint64_t)T}, strides[1] = {(cuuint64_t)line_pitch(2ll * I) * 2};
-    const cuuint32_t box[2] = {32, 32}, ones[2] = {1, 1};
-    for (int half = 0; half < 2 && ok; ++half)
-        ok = h->e.encode(&g.job[1 + half].d, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dgu + (size_t)half * I * 2, dims, strides, box, ones,
-                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const int rows_a = gemm_rows(T);
+    const long long h_pitch = line_pitch(I), dgu_pitch = line_pitch(2ll * I);
+    bool ok = map_k(h->e, g.job[0].a, WEAVE_BF16, dy, T, H, rows_a) && map_mn(h->e, g.job[0].b[0], h->cfg.down, H, I) &&
+              map_k(h->e, g.job[1].a, WEAVE_BF16, x, T, H, rows_a) && map_k(h->e, g.job[1].b[0], WEAVE_BF16, h->cfg.gate_up, I, H, wide) &&
+              map_k(h->e, g.job[1].b[1], WEAVE_BF16, up, I, H, wide);
     if (!ok) return WEAVE_ERR_CUDA;
     g.job[0].b[1] = g.job[0].b[0];
-    gemm_job(g.job[0], T, I, H, 64, wide, false, false);
-    gemm_job(g.job[1], T, I, H, 64, wide, false, false);
+    // d(gate) and d(up) lie side by side in rows of 2I
+    gemm_job(g.job[0], T, I, H, 64, wide, false, false, hbuf, h_pitch);
+    gemm_job(g.job[1], T, I, H, 64, wide, false, false, dgu, dgu_pitch);
+    gemm_job(g.job[2], T, I, H, 64, wide, false, false, dgu + (size_t)I * 2, dgu_pitch);
     err = launch_gemm<kEpiGrad, false>(h->e, g, 1, wide * 128, kPlain, stream);
     if (err != cudaSuccess) return cuda_fail(h->e, err);
     // dx = [dg du] W_gu, dW_gu = [dg du]^T x, dW_d = dy^T h: one launch, so that their last waves fill one another
     GemmArgs d;
-    ok = map_k(h->e, d.job[0].a, WEAVE_BF16, dgu, T, 2ll * I, 128, line_pitch(2ll * I)) && map_mn(h->e, d.job[0].b[0], h->cfg.gate_up, 2ll * I, H) &&
-         map_d(h->e, d.job[0], dx, T, H) && map_mn(h->e, d.job[1].a, dgu, T, 2ll * I, line_pitch(2ll * I)) &&
-         map_mn(h->e, d.job[1].b[0], x, T, H) && map_d(h->e, d.job[1], dgate_up, 2ll * I, H) &&
-         map_mn(h->e, d.job[2].a, dy, T, H) && map_mn(h->e, d.job[2].b[0], hbuf, T, I, line_pitch(I)) && map_d(h->e, d.job[2], ddown, H, I);
+    ok = map_k(h->e, d.job[0].a, WEAVE_BF16, dgu, T, 2ll * I, rows_a, dgu_pitch) && map_mn(h->e, d.job[0].b[0], h->cfg.gate_up, 2ll * I, H) &&
+         map_mn(h->e, d.job[1].a, dgu, T, 2ll * I, dgu_pitch) && map_mn(h->e, d.job[1].b[0], x, T, H) &&
+         map_mn(h->e, d.job[2].a, dy, T, H) && map_mn(h->e, d.job[2].b[0], hbuf, T, I, h_pitch);
     if (!ok) return WEAVE_ERR_CUDA;
     for (int i = 0; i < 3; ++i) d.job[i].b[1] = d.job[i].b[0];
     const double others = (gemm_tiles(2 * I, H, 256) + gemm_tiles(H, I, 256)) * gemm_tile_us((T + 63) / 64, 256);
-    gemm_job(d.job[0], T, H, 2ll * I, 64, gemm_width_among(h->e, T, H, (2 * I + 63) / 64, others), false, true);
-    gemm_job(d.job[1], 2 * I, H, T, 64, 256, true, true);
-    gemm_job(d.job[2], H, I, T, 64, 256, true, true);
+    gemm_job(d.job[0], T, H, 2ll * I, 64, gemm_width_among(h->e, T, H, (2 * I + 63) / 64, others), false, true, dx, H);
+    gemm_job(d.job[1], 2 * I, H, T, 64, 256, true, true, dgate_up, H);
+    gemm_job(d.job[2], H, I, T, 64, 256, true, true, ddown, I);
     err = launch_gemm<kEpiStore, false>(h->e, d, 3, kGemmHalf, kBehind, stream);
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }
@@ -699,7 +700,7 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     const void *q = round ? xq : x;
     if (round) x_scale = xs;
     const bool direct = (size_t)N * out_size % 16 != 0;
-    const GemmWidth w = gemm_width(h->e, T, N, (K + 127) / 128, 256, out_type == WEAVE_F32 && !direct ? 32 : 16, 1);
+    const GemmWidth w = gemm_width(h->e, T, N, (K + 127) / 128, 256, 16, 1);
     if (T <= kSmallMaxT && small_wins(T, 1, round, small_us(h->e, N, false, K, 128, T), w.us)) {
         SmallArgs a;
         a.products = 0;
@@ -716,16 +717,14 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     }
     GemmArgs g;
     const int wide = w.width;
+    const int rows_a = gemm_rows(T);
     g.direct = direct;
     g.out_f32 = out_type == WEAVE_F32;
-    g.out = out;
-    g.ld_out = N;
     g.row_scale = x_scale;
     g.col_scale = h->cfg.scale;
-    if (!map_k(h->e, g.job[0].a, WEAVE_INT8, q, T, K) || !map_k(h->e, g.job[0].b[0], WEAVE_INT8, h->cfg.weight, N, K, wide / 2)) return WEAVE_ERR_CUDA;
-    if (!g.direct && !(g.out_f32 ? map_2d(h->e, g.job[0].d, WEAVE_F32, out, T, N, 32, 32) : map_d(h->e, g.job[0], out, T, N))) return WEAVE_ERR_CUDA;
+    if (!map_k(h->e, g.job[0].a, WEAVE_INT8, q, T, K, rows_a) || !map_k(h->e, g.job[0].b[0], WEAVE_INT8, h->cfg.weight, N, K, wide / 2)) return WEAVE_ERR_CUDA;
     g.job[0].b[1] = g.job[0].b[0];
-    gemm_job(g.job[0], T, N, K, 128, wide, false, false);
+    gemm_job(g.job[0], T, N, K, 128, wide, false, false, out, N);
     err = launch_gemm<kEpiScaled, true>(h->e, g, 1, wide * 64, round ? kBehind : kPlain, stream);
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }

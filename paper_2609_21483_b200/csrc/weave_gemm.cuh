@@ -10,7 +10,7 @@
 //   kEpiScaledGated h as above from scaled g and u (128)                                 8-bit integers, K-major
 //
 // A tile is 256 rows of A (128 per CTA) by up to 256 accumulator columns (fewer where that fills the last wave).  A k-step
-// is 128 bytes of K (64 bf16 or 128 8-bit integers): 16 KB of A and up to 16 KB of B per CTA, 192 KB of them in flight.  Rows, columns and K that stick out over
+// is 128 bytes of K (64 bf16 or 128 8-bit integers): up to 16 KB of A and of B per CTA, 192 KB of them in flight.  Rows, columns and K that stick out over
 // the matrices are zero-filled by the tensor maps on the way in and clipped by them on the way out.
 //
 // Bound: the tensor pipe (256 x 256 x 16 takes 128 cycles) and, over more than some milliseconds, the power limit.
@@ -120,14 +120,6 @@ __device__ __forceinline__ void ffn_mma_kstep_pair(uint32_t d_tmem, uint64_t a_d
 #undef WEAVE_KSTEP_PAIR
 }
 
-// shared -> global through a tensor map (clips what sticks out), tracked by the thread's bulk async-groups
-__device__ __forceinline__ void tma_store_2d(const void *map, uint32_t smem_src, int x, int row)
-{
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(smem_src), "r"(x),
-                 "r"(row)
-                 : "memory");
-}
-
 // ------------------------------------------------------------------------------------ the activation
 
 // s = sigmoid(g).  exp overflows to inf for g below -88, where s is 0 either way; NaN and +inf come through.
@@ -143,13 +135,14 @@ __device__ __forceinline__ float gated(float g, float u) { return g * fast_sigmo
 struct alignas(64) GemmJob {
     CUtensorMap a;
     CUtensorMap b[2];        // [rank of the CTA in its pair]: the gated forms give gate rows to one, up rows to the other
-    CUtensorMap d;           // results; kEpiGrad: h, dg, du in jobs 0, 1, 2
-    CUtensorMap d8;          // results in bf16, eight columns at a time: what a width leaves over 64
+    void *out;               // result, rows `ld` elements apart; kEpiGrad: h, dg, du in jobs 0, 1, 2
+    long long ld;
     int M, N;                // rows and columns of the result
     int ksteps;
     int a_mn, b_mn;          // kEpiStore: operand is MN-major
-    int width;               // columns of the result in a tile: a multiple of 16 up to 256, gated of 8 up to 128; of 32 where
-                             // the result is in fp32, of 64 where B is MN-major (kEpiGrad, too): with 16 of them in a CTA
+    int rows;                // rows of A that a CTA takes of a tile, a multiple of 8 up to 128: a tile is 2 x rows high
+    int width;               // columns of the result in a tile: a multiple of 16 up to 256, gated of 8 up to 128; of
+                             // 64 where B is MN-major (kEpiGrad, too): with 16 of them in a CTA
                              // the products came out wrong, with 32 right
     int tiles_m, tiles_n, group_m;
 };
@@ -160,21 +153,18 @@ struct alignas(64) GemmArgs {
     unsigned long long timeout_ns;
     const float *row_scale;  // scaled forms: [M] and [N] (gated: [2N], gate then up)
     const float *col_scale;
-    void *out;               // kEpiScaled, for rows that no tensor map can describe
-    long long ld_out;
-    int out_f32, direct;     // kEpiScaled: type of the result; 1 = ordinary stores (row length not a multiple of 16 bytes)
+    int out_f32, direct;     // kEpiScaled: type of the result; 1 = row length not a multiple of 16 bytes
     int extra;               // kEpiStore: see gemm_tile()
-    int stages, stage_bytes;
+    int stages, a_bytes, stage_bytes;
 };
 
-constexpr int kGemmThreads = 256;
-constexpr int kGemmMaxStages = 9;
-constexpr int kGemmHalf = 16384;                    // A's bytes of one k-step in one CTA, B's at most
+constexpr int kGemmThreads = 384;                   // two producers, the issuer, one idle warp, eight epilogue warps
+constexpr int kGemmMaxStages = 12;
+constexpr int kGemmHalf = 16384;                    // A's or B's bytes of one k-step in one CTA, at most
 constexpr int kGemmRing = 6 * 2 * kGemmHalf;
-constexpr int kGemmStaging = 8192;                  // per epilogue warp
+constexpr int kGemmStaging = 4096;                  // per epilogue warp
 constexpr int kGemmSmemStaging = kGemmRing;
-constexpr int kGemmSmemScales = kGemmSmemStaging + 4 * kGemmStaging;
-constexpr int kGemmSmemBars = kGemmSmemScales + 4 * 256;
+constexpr int kGemmSmemBars = kGemmSmemStaging + 8 * kGemmStaging;
 constexpr int kGemmSmemBytes = kGemmSmemBars + 256 + 1024;      // 1024: the stages start on a swizzle atom's boundary
 static_assert(kGemmSmemBytes <= 232448, "227 KB per CTA");
 
@@ -195,7 +185,7 @@ __device__ __forceinline__ void gemm_tile_at(const GemmJob &p, int t, GemmTile &
     const int g = t / per, r = t - g * per;
     const int gm = min(p.group_m, p.tiles_m - g * p.group_m);
     const int n = r / gm;
-    at.m0 = (g * p.group_m + r - n * gm) * 256;
+    at.m0 = (g * p.group_m + r - n * gm) * 2 * p.rows;
     at.n0 = n * p.width;
 }
 
@@ -227,25 +217,30 @@ __device__ __forceinline__ bool gemm_tile(const GemmArgs &p, int i, int pair, in
     return true;
 }
 
-// A warp's 32 rows x 64 columns in bf16 on their way out: 128-byte rows, swizzled, for one tensor copy; of a narrower rest
-// of a tile eight columns lie together, for copies of their own.
-__device__ __forceinline__ uint32_t gemm_staged(uint32_t dst, int lane, int j, int there)
+// A warp's 32 rows of kRow bytes on their way out: staged by lane = row with 16-byte chunks swizzled (no bank conflicts
+// either way), stored with the lanes of a row side by side, whole 128-byte lines at a time.  (Tensor-map stores from the
+// same place took 2.4 us per tile of 256 x 256 instead of 1.2: a copy costs its thread 130 ns, and the next one waits.)
+// rows, bytes: how much of it is there, bytes a multiple of 16.
+template <int kRow>
+__device__ __forceinline__ uint32_t gemm_staged(uint32_t stage, int row, int chunk)
 {
-    return there == 64 ? dst + lane * 128 + ((j ^ (lane & 7)) << 4) : dst + j * 512 + lane * 16;
+    if constexpr (kRow == 128) return stage + row * 128 + ((chunk ^ (row & 7)) << 4);
+    else return stage + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
 }
-__device__ __forceinline__ void gemm_store_bf16(const GemmJob &job, uint32_t src, int lane, int col, int row0, int there, bool any_row)
+template <int kRow>
+__device__ __forceinline__ void gemm_store_rows(void *to, long long pitch_bytes, int rows, int bytes, uint32_t stage, int lane)
 {
-    fence_proxy_async_shared();
+    constexpr int kLanes = kRow / 16, kRows = 32 / kLanes;
+    const int chunk = lane % kLanes, first = lane / kLanes;
     __syncwarp();
-    if (lane == 0) {
-        if (any_row) {
-            if (there == 64) {
-                if (col < job.N) tma_store_2d(&job.d, src, col, row0);
-            } else {
-                for (int j = 0; j * 8 < there && col + j * 8 < job.N; ++j) tma_store_2d(&job.d8, src + j * 512, col + j * 8, row0);
-            }
+    if (chunk * 16 < bytes) {
+        uint8_t *at = static_cast<uint8_t *>(to) + first * pitch_bytes + chunk * 16;
+#pragma unroll
+        for (int i = 0; i < 32 / kRows; ++i) {
+            const int row = first + i * kRows;
+            if (row < rows) *reinterpret_cast<uint4 *>(at) = ld_shared_v4(gemm_staged<kRow>(stage, row, chunk));
+            at += kRows * pitch_bytes;
         }
-        bulk_commit();
     }
 }
 
@@ -269,7 +264,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int i = 0; i < kGemmMaxStages; ++i) { mbar_init(&bars.full[i], 1); mbar_init(&bars.empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&bars.acc_full[i], 1); mbar_init(&bars.acc_empty[i], 8); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&bars.acc_full[i], 1); mbar_init(&bars.acc_empty[i], 16); }
         fence_mbar_init();
     }
     if (warp == 3) { tmem_alloc_pair(&bars.tmem_base, 512); tmem_relinquish_pair(); }
@@ -285,6 +280,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
         // to the full barrier in the pair's leader
         const bool load_a = warp == 0;
         pdl_wait();
+        fence_proxy_async_global();      // what the launch before wrote with ordinary stores is read by tensor copies
         int s = 0;
         uint32_t ph = 0;
         for (int i = 0; ok && gemm_tile<kJobs>(p, i, pair, pairs, at); ++i) {
@@ -294,16 +290,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                 const bool a_mn = kJobs && job.a_mn, b_mn = kJobs ? job.b_mn != 0 : dh;
                 const int half = kGatedTile && !dh ? job.width : job.width / 2;          // this CTA's rows of B
                 const int b_boxes = b_mn ? (half + 63) / 64 : 1;
-                const uint32_t tx = 2u * (kGemmHalf + (b_mn ? (uint32_t)b_boxes * 8192u : (uint32_t)half * 128u));
+                const uint32_t tx = 2u * ((uint32_t)job.rows * 128u + (b_mn ? (uint32_t)b_boxes * 8192u : (uint32_t)half * 128u));
                 const void *map = load_a ? &job.a : &job.b[rank];
-                const int mn = load_a ? at.m0 + (int)rank * 128 : at.n0 + (kGatedTile && !dh ? 0 : (int)rank * half);
+                const int mn = load_a ? at.m0 + (int)rank * job.rows : at.n0 + (kGatedTile && !dh ? 0 : (int)rank * half);
                 const bool mn_major = load_a ? a_mn : b_mn;
                 const bool second = load_a ? a_mn : b_boxes == 2;
                 const int ks = job.ksteps;
                 for (int k = 0; k < ks; ++k) {
                     ok = __all_sync(0xffffffffu, ffn_wait(&bars.empty[s], ph ^ 1u, wc, 1 + warp));
                     if (!ok) break;
-                    const uint32_t dst = smem + s * p.stage_bytes + (load_a ? 0 : kGemmHalf);
+                    const uint32_t dst = smem + s * p.stage_bytes + (load_a ? 0 : p.a_bytes);
                     const uint32_t full = mapa_u32(smem_u32(&bars.full[s]), 0);
                     if (elect_one()) {
                         if (load_a && rank == 0) mbar_arrive_expect_tx(&bars.full[s], tx);
@@ -345,7 +341,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                         ok = __all_sync(0xffffffffu, ffn_wait(&bars.full[s], ph, wc, 4));
                         if (!ok) break;
                         tc_fence_after();
-                        const uint32_t a = smem + s * p.stage_bytes, b = a + kGemmHalf;
+                        const uint32_t a = smem + s * p.stage_bytes, b = a + p.a_bytes;      // (128 rows are read from a on, whatever lies there)
                         ffn_mma_kstep_pair<kI8>(d, a_mn ? umma_desc_mn_sw128(a) : umma_desc_sw128(a),
                                                 b_mn ? umma_desc_mn_sw128(b) : umma_desc_sw128(b), a_inc, b_inc, idesc, (uint32_t)(k != 0),
                                                 &bars.empty[s]);
@@ -358,38 +354,49 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
             if (!ok) ffn_linger();
         }
     } else if (warp >= 4) {
-        // ---- epilogue: each warp the 32 accumulator lanes of its quarter; rows m0 + 128 rank + 32 quarter + lane
-        const int quarter = warp - 4;
+        // ---- epilogue: each warp the 32 accumulator lanes of its quarter, this CTA's rows from 32 quarter on; two warps
+        // share a quarter, 64 columns (kEpiGrad: 32) in turn
+        const int quarter = warp & 3, group = (warp - 4) >> 2;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
-        const uint32_t stage = smem + kGemmSmemStaging + quarter * kGemmStaging;
-        float *const scales = reinterpret_cast<float *>(smem_g + kGemmSmemScales + quarter * 256);
+        const uint32_t stage = smem + kGemmSmemStaging + (warp - 4) * kGemmStaging;
+        float *const scales = reinterpret_cast<float *>(smem_g + kGemmSmemStaging + (warp - 4) * kGemmStaging);      // before results lie there
         const uint32_t empty0 = mapa_u32(smem_u32(&bars.acc_empty[0]), 0);
         pdl_wait();
-        uint32_t slot = 0;          // half of the staging buffer that is written next (not kEpiGrad)
         for (int n = 0; gemm_tile<kJobs>(p, n, pair, pairs, at); ++n) {
             const GemmJob &job = p.job[at.job];
-            const int M = job.M, N = job.N, width = job.width, n0 = at.n0;
-            const int row0 = at.m0 + (int)rank * 128 + quarter * 32;
-            const int buf = n & 1;
+            const int N = job.N, width = job.width, n0 = at.n0, buf = n & 1;
+            const int row0 = at.m0 + (int)rank * job.rows + quarter * 32;
+            const int rows = min(min(32, job.rows - quarter * 32), job.M - row0);       // the warp's; may be none
             ok = __all_sync(0xffffffffu, ffn_wait(&bars.acc_full[buf], (n >> 1) & 1, wc, 5));
             if (!ok) break;
             tc_fence_after();
-            const bool any_row = row0 < M;       // whole warp
+            // accumulator read: hand it back to the pair's issuer
+            const auto release = [&]() {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote(kEpi == kEpiGrad ? empty0 : empty0 + buf * 8);
+            };
+            if (rows <= 0) {
+                release();
+                continue;
+            }
             float sx = 0.0f;
-            if constexpr (kI8) sx = row0 + lane < M ? p.row_scale[row0 + lane] : 0.0f;
+            if constexpr (kI8) sx = lane < rows ? p.row_scale[row0 + lane] : 0.0f;
 
             if constexpr (kEpi == kEpiStore || kEpi == kEpiScaled) {
+                const int last = min((width - 1) / 64, (N - 1 - n0) / 64);
+                if (group > last) release();
 #pragma unroll 1
-                for (int c = 0; c * 64 < width; ++c) {
-                    const int col = n0 + c * 64, there = min(64, width - c * 64);
+                for (int c = group; c <= last; c += 2) {
+                    const int col = n0 + c * 64, cols = min(min(64, width - c * 64), N - col);
                     uint32_t v[64];
                     tmem_ld_32x64(lane_base + buf * 256 + c * 64, v);
                     tmem_ld_wait64(v);
-                    if (!any_row || col >= N) continue;
+                    if (c + 2 > last) release();
                     if constexpr (kEpi == kEpiScaled) {
                         __syncwarp();
-                        scales[lane] = col + lane < N ? p.col_scale[col + lane] : 0.0f;
-                        scales[lane + 32] = col + 32 + lane < N ? p.col_scale[col + 32 + lane] : 0.0f;
+                        scales[lane] = lane < cols ? p.col_scale[col + lane] : 0.0f;
+                        scales[lane + 32] = lane + 32 < cols ? p.col_scale[col + 32 + lane] : 0.0f;
                         __syncwarp();
 #pragma unroll
                         for (int i = 0; i < 64; i += 4) {
@@ -402,69 +409,56 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                     }
                     const bool f32 = kEpi == kEpiScaled && p.out_f32;
                     if (kEpi == kEpiScaled && p.direct) {
-                        // row by row through shared memory, so that a warp's stores lie side by side
-                        float *const out_f = static_cast<float *>(p.out);
-                        __nv_bfloat16 *const out_b = static_cast<__nv_bfloat16 *>(p.out);
+                        // rows that start anywhere: a warp's stores of one row lie side by side
+                        float *const out_f = static_cast<float *>(job.out);
+                        __nv_bfloat16 *const out_b = static_cast<__nv_bfloat16 *>(job.out);
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
                             __syncwarp();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) st_shared_u32(stage + lane * 132 + i * 4, v[half * 32 + i]);
+                            for (int i = 0; i < 32; ++i) st_shared_u32(stage + lane * 128 + ((i ^ lane) << 2), v[half * 32 + i]);
                             __syncwarp();
-                            const int cc = half * 32 + lane < there ? col + half * 32 + lane : N;
-                            const int rows = min(32, M - row0);
-                            if (cc < N)
+                            const int cc = half * 32 + lane;
+                            if (cc < cols)
 #pragma unroll 8
                                 for (int r = 0; r < rows; ++r) {
-                                    const float y = ld_shared_f32(stage + r * 132 + lane * 4);
-                                    const long long at = (long long)(row0 + r) * p.ld_out + cc;
-                                    if (f32) out_f[at] = y;
-                                    else out_b[at] = __float2bfloat16_rn(y);
+                                    const float y = ld_shared_f32(stage + r * 128 + ((lane ^ r) << 2));
+                                    const long long to = (long long)(row0 + r) * job.ld + col + cc;
+                                    if (f32) out_f[to] = y;
+                                    else out_b[to] = __float2bfloat16_rn(y);
                                 }
                         }
-                        continue;
-                    }
-                    if (f32) {
-                        // two tiles of 32 rows x 32 columns, one in each half of the staging buffer
+                    } else if (f32) {
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
-                            if (lane == 0) bulk_wait_read<1>();
                             __syncwarp();
-                            const uint32_t dst = stage + half * 4096;
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
-                                st_shared_v4(dst + lane * 128 + ((j ^ (lane & 7)) << 4),
-                                             make_uint4(v[half * 32 + j * 4], v[half * 32 + j * 4 + 1], v[half * 32 + j * 4 + 2],
-                                                        v[half * 32 + j * 4 + 3]));
-                            fence_proxy_async_shared();
-                            __syncwarp();
-                            if (lane == 0 && half * 32 < there && col + half * 32 < N) tma_store_2d(&job.d, dst, col + half * 32, row0);
-                            if (lane == 0) bulk_commit();
+                                st_shared_v4(gemm_staged<128>(stage, lane, j), make_uint4(v[half * 32 + j * 4], v[half * 32 + j * 4 + 1],
+                                                                                       v[half * 32 + j * 4 + 2], v[half * 32 + j * 4 + 3]));
+                            gemm_store_rows<128>(static_cast<float *>(job.out) + row0 * job.ld + col + half * 32, job.ld * 4, rows,
+                                                 (cols - half * 32) * 4, stage, lane);
                         }
                     } else {
-                        if (lane == 0) bulk_wait_read<1>();
                         __syncwarp();
-                        const uint32_t dst = stage + slot * 4096;
-                        slot ^= 1u;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             uint32_t w[4];
 #pragma unroll
                             for (int q = 0; q < 4; ++q)
                                 w[q] = pack_bf16x2(__uint_as_float(v[j * 8 + q * 2]), __uint_as_float(v[j * 8 + q * 2 + 1]));
-                            st_shared_v4(gemm_staged(dst, lane, j, there), make_uint4(w[0], w[1], w[2], w[3]));
+                            st_shared_v4(gemm_staged<128>(stage, lane, j), make_uint4(w[0], w[1], w[2], w[3]));
                         }
-                        gemm_store_bf16(job, dst, lane, col, row0, there, true);
+                        gemm_store_rows<128>(static_cast<__nv_bfloat16 *>(job.out) + row0 * job.ld + col, job.ld * 2, rows, cols * 2, stage, lane);
                     }
                 }
             } else if constexpr (kEpi == kEpiGated || kEpi == kEpiScaledGated) {
+                const int last = min((width - 1) / 64, (N - 1 - n0) / 64);
+                if (group > last) release();
 #pragma unroll 1
-                for (int c = 0; c * 64 < width; ++c) {
-                    const int there = min(64, width - c * 64);
-                    const uint32_t dst = stage + slot * 4096;
-                    slot ^= 1u;
-                    if (lane == 0) bulk_wait_read<1>();
-                    __syncwarp();
+                for (int c = group; c <= last; c += 2) {
+                    const int col = n0 + c * 64, cols = min(min(64, width - c * 64), N - col);
+                    uint32_t packed[32];
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const int cc = c * 64 + half * 32;
@@ -473,11 +467,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                         tmem_ld_32x32(lane_base + buf * 256 + width + cc, u);
                         tmem_ld_wait32(g);
                         reg_fence32(u);
+                        if (c + 2 > last && half == 1) release();
                         if constexpr (kEpi == kEpiScaledGated) {
-                            const int col = n0 + cc + lane;
+                            const bool there = half * 32 + lane < cols;
                             __syncwarp();
-                            scales[lane] = col < N ? p.col_scale[col] : 0.0f;
-                            scales[lane + 32] = col < N ? p.col_scale[N + col] : 0.0f;
+                            scales[lane] = there ? p.col_scale[n0 + cc + lane] : 0.0f;
+                            scales[lane + 32] = there ? p.col_scale[N + n0 + cc + lane] : 0.0f;
                             __syncwarp();
 #pragma unroll
                             for (int i = 0; i < 32; i += 4) {
@@ -492,25 +487,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                             }
                         }
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                const int i = j * 8 + q * 2;
-                                w[q] = pack_bf16x2(gated(__uint_as_float(g[i]), __uint_as_float(u[i])),
-                                                   gated(__uint_as_float(g[i + 1]), __uint_as_float(u[i + 1])));
-                            }
-                            st_shared_v4(gemm_staged(dst, lane, half * 4 + j, there), make_uint4(w[0], w[1], w[2], w[3]));
-                        }
+                        for (int i = 0; i < 16; ++i)
+                            packed[half * 16 + i] = pack_bf16x2(gated(__uint_as_float(g[2 * i]), __uint_as_float(u[2 * i])),
+                                                                gated(__uint_as_float(g[2 * i + 1]), __uint_as_float(u[2 * i + 1])));
                     }
-                    gemm_store_bf16(job, dst, lane, n0 + c * 64, row0, there, any_row);
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        st_shared_v4(gemm_staged<128>(stage, lane, j), make_uint4(packed[j * 4], packed[j * 4 + 1], packed[j * 4 + 2], packed[j * 4 + 3]));
+                    gemm_store_rows<128>(static_cast<__nv_bfloat16 *>(job.out) + row0 * job.ld + col, job.ld * 2, rows, cols * 2, stage, lane);
                 }
             } else {
-                // kEpiGrad: 32 columns at a time, three results of 32 x 32 bf16 (64-byte swizzle) in rotating quarters
-                // of the staging buffer
-                int quad = 0;
+                const int last = min(width / 32 - 1, (N - 1 - n0) / 32);
+                if (group > last) release();
 #pragma unroll 1
-                for (int c = 0; c < width / 32; ++c) {
+                for (int c = group; c <= last; c += 2) {
+                    const int col = n0 + c * 32, cols = min(32, N - col);
                     uint32_t g[32], u[32], d[32];
                     tmem_ld_32x32(lane_base + c * 32, g);
                     tmem_ld_32x32(lane_base + width + c * 32, u);
@@ -518,45 +510,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                     tmem_ld_wait32(g);
                     reg_fence32(u);
                     reg_fence32(d);
+                    if (c + 2 > last) release();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const float fg = __uint_as_float(g[i]), fu = __uint_as_float(u[i]), fd = __uint_as_float(d[i]);
-                        const float sg = fast_sigmoid(fg);
-                        const float si = fg * sg;
-                        g[i] = __float_as_uint(si * fu);                                    // h
-                        u[i] = __float_as_uint(fd * fu * sg * (1.0f + fg * (1.0f - sg)));   // dg
-                        d[i] = __float_as_uint(fd * si);                                    // du
+                    for (int i = 0; i < 32; i += 2) {
+                        float r[3][2];
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const float fg = __uint_as_float(g[i + q]), fu = __uint_as_float(u[i + q]), fd = __uint_as_float(d[i + q]);
+                            const float sg = fast_sigmoid(fg), si = fg * sg;
+                            r[0][q] = si * fu;                                         // h
+                            r[1][q] = fd * fu * sg * (1.0f + fg * (1.0f - sg));        // dg
+                            r[2][q] = fd * si;                                         // du
+                        }
+                        g[i / 2] = pack_bf16x2(r[0][0], r[0][1]);
+                        u[i / 2] = pack_bf16x2(r[1][0], r[1][1]);
+                        d[i / 2] = pack_bf16x2(r[2][0], r[2][1]);
                     }
 #pragma unroll
-                    for (int which = 0; which < 3; ++which) {
-                        const uint32_t *v = which == 0 ? g : which == 1 ? u : d;
-                        const uint32_t dst = stage + quad * 2048;
-                        quad = (quad + 1) & 3;
-                        if (lane == 0) bulk_wait_read<3>();
+                    for (int w = 0; w < 3; ++w) {
+                        const uint32_t *v = w == 0 ? g : w == 1 ? u : d;
+                        const GemmJob &to = p.job[w];
                         __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int q = 0; q < 4; ++q)
-                                w[q] = pack_bf16x2(__uint_as_float(v[j * 8 + q * 2]), __uint_as_float(v[j * 8 + q * 2 + 1]));
-                            st_shared_v4(dst + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
-                        }
-                        fence_proxy_async_shared();
-                        __syncwarp();
-                        if (lane == 0) {
-                            if (any_row && n0 + c * 32 < N) tma_store_2d(&p.job[which].d, dst, n0 + c * 32, row0);
-                            bulk_commit();
-                        }
+                        for (int j = 0; j < 4; ++j)
+                            st_shared_v4(gemm_staged<64>(stage, lane, j), make_uint4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]));
+                        gemm_store_rows<64>(static_cast<__nv_bfloat16 *>(to.out) + row0 * to.ld + col, to.ld * 2, rows, cols * 2, stage, lane);
                     }
                 }
             }
-            // accumulator read: hand it back to the pair's issuer
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_remote(kEpi == kEpiGrad ? empty0 : empty0 + buf * 8);
         }
-        if (lane == 0) bulk_wait<0>();
         if (!ok) ffn_linger();
     }
     __syncwarp();
