@@ -217,32 +217,31 @@ __device__ __forceinline__ bool gemm_tile(const GemmArgs &p, int i, int pair, in
     return true;
 }
 
-// A warp's 32 rows of kRow bytes on their way out: staged by lane = row with 16-byte chunks swizzled (no bank conflicts
+// 32 rows of 128 bytes on their way out: staged by lane = row with 16-byte chunks swizzled (no bank conflicts
 // either way), stored with the lanes of a row side by side, whole 128-byte lines at a time.  (Tensor-map stores from the
 // same place took 2.4 us per tile of 256 x 256 instead of 1.2: a copy costs its thread 130 ns, and the next one waits.)
 // rows, bytes: how much of it is there, bytes a multiple of 16.
-template <int kRow>
 __device__ __forceinline__ uint32_t gemm_staged(uint32_t stage, int row, int chunk)
 {
-    if constexpr (kRow == 128) return stage + row * 128 + ((chunk ^ (row & 7)) << 4);
-    else return stage + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
+    return stage + row * 128 + ((chunk ^ (row & 7)) << 4);
 }
-template <int kRow>
-__device__ __forceinline__ void gemm_store_rows(void *to, long long pitch_bytes, int rows, int bytes, uint32_t stage, int lane)
+// kTimes x 4 rows from row `first` on
+template <int kTimes>
+__device__ __forceinline__ void gemm_store_rows(void *to, long long pitch_bytes, int rows, int bytes, uint32_t stage, int lane, int first)
 {
-    constexpr int kLanes = kRow / 16, kRows = 32 / kLanes;
-    const int chunk = lane % kLanes, first = lane / kLanes;
-    __syncwarp();
+    const int chunk = lane & 7, mine = first + (lane >> 3);
     if (chunk * 16 < bytes) {
-        uint8_t *at = static_cast<uint8_t *>(to) + first * pitch_bytes + chunk * 16;
+        uint8_t *at = static_cast<uint8_t *>(to) + mine * pitch_bytes + chunk * 16;
 #pragma unroll
-        for (int i = 0; i < 32 / kRows; ++i) {
-            const int row = first + i * kRows;
-            if (row < rows) *reinterpret_cast<uint4 *>(at) = ld_shared_v4(gemm_staged<kRow>(stage, row, chunk));
-            at += kRows * pitch_bytes;
+        for (int i = 0; i < kTimes; ++i) {
+            const int row = mine + i * 4;
+            if (row < rows) *reinterpret_cast<uint4 *>(at) = ld_shared_v4(gemm_staged(stage, row, chunk));
+            at += 4 * pitch_bytes;
         }
     }
 }
+// 64 threads in two whole warps
+__device__ __forceinline__ void barrier_sync_64(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
 template <int kEpi, bool kI8>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) weave_gemm_kernel(const __grid_constant__ GemmArgs p)
@@ -355,7 +354,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
         }
     } else if (warp >= 4) {
         // ---- epilogue: each warp the 32 accumulator lanes of its quarter, this CTA's rows from 32 quarter on; two warps
-        // share a quarter, 64 columns (kEpiGrad: 32) in turn
+        // share a quarter, 64 columns in turn
         const int quarter = warp & 3, group = (warp - 4) >> 2;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
         const uint32_t stage = smem + kGemmSmemStaging + (warp - 4) * kGemmStaging;
@@ -434,10 +433,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                             __syncwarp();
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
-                                st_shared_v4(gemm_staged<128>(stage, lane, j), make_uint4(v[half * 32 + j * 4], v[half * 32 + j * 4 + 1],
+                                st_shared_v4(gemm_staged(stage, lane, j), make_uint4(v[half * 32 + j * 4], v[half * 32 + j * 4 + 1],
                                                                                        v[half * 32 + j * 4 + 2], v[half * 32 + j * 4 + 3]));
-                            gemm_store_rows<128>(static_cast<float *>(job.out) + row0 * job.ld + col + half * 32, job.ld * 4, rows,
-                                                 (cols - half * 32) * 4, stage, lane);
+                            __syncwarp();
+                            gemm_store_rows<8>(static_cast<float *>(job.out) + row0 * job.ld + col + half * 32, job.ld * 4, rows,
+                                               (cols - half * 32) * 4, stage, lane, 0);
                         }
                     } else {
                         __syncwarp();
@@ -447,9 +447,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
 #pragma unroll
                             for (int q = 0; q < 4; ++q)
                                 w[q] = pack_bf16x2(__uint_as_float(v[j * 8 + q * 2]), __uint_as_float(v[j * 8 + q * 2 + 1]));
-                            st_shared_v4(gemm_staged<128>(stage, lane, j), make_uint4(w[0], w[1], w[2], w[3]));
+                            st_shared_v4(gemm_staged(stage, lane, j), make_uint4(w[0], w[1], w[2], w[3]));
                         }
-                        gemm_store_rows<128>(static_cast<__nv_bfloat16 *>(job.out) + row0 * job.ld + col, job.ld * 2, rows, cols * 2, stage, lane);
+                        __syncwarp();
+                        gemm_store_rows<8>(static_cast<__nv_bfloat16 *>(job.out) + row0 * job.ld + col, job.ld * 2, rows, cols * 2, stage, lane, 0);
                     }
                 }
             } else if constexpr (kEpi == kEpiGated || kEpi == kEpiScaledGated) {
@@ -494,23 +495,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                     __syncwarp();
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        st_shared_v4(gemm_staged<128>(stage, lane, j), make_uint4(packed[j * 4], packed[j * 4 + 1], packed[j * 4 + 2], packed[j * 4 + 3]));
-                    gemm_store_rows<128>(static_cast<__nv_bfloat16 *>(job.out) + row0 * job.ld + col, job.ld * 2, rows, cols * 2, stage, lane);
+                        st_shared_v4(gemm_staged(stage, lane, j), make_uint4(packed[j * 4], packed[j * 4 + 1], packed[j * 4 + 2], packed[j * 4 + 3]));
+                    __syncwarp();
+                    gemm_store_rows<8>(static_cast<__nv_bfloat16 *>(job.out) + row0 * job.ld + col, job.ld * 2, rows, cols * 2, stage, lane, 0);
                 }
             } else {
-                const int last = min(width / 32 - 1, (N - 1 - n0) / 32);
-                if (group > last) release();
+                // 64 columns at a time, 32 of them by each of a quarter's two warps, which stage a result's rows side by side
+                // and store half of them each: whole lines.  Two places in turn; a place's readers have met at the barrier
+                // of the other one
+                const int last = (min(width, N - n0) - 1) / 64;
+                const uint32_t place = smem + kGemmSmemStaging + quarter * kGemmStaging;
+                uint32_t turn = 0;
 #pragma unroll 1
-                for (int c = group; c <= last; c += 2) {
-                    const int col = n0 + c * 32, cols = min(32, N - col);
+                for (int c = 0; c <= last; ++c) {
+                    const int from = c * 64 + group * 32, col = n0 + c * 64, cols = min(64, N - col);
                     uint32_t g[32], u[32], d[32];
-                    tmem_ld_32x32(lane_base + c * 32, g);
-                    tmem_ld_32x32(lane_base + width + c * 32, u);
-                    tmem_ld_32x32(lane_base + 256 + buf * 128 + c * 32, d);
+                    tmem_ld_32x32(lane_base + from, g);
+                    tmem_ld_32x32(lane_base + width + from, u);
+                    tmem_ld_32x32(lane_base + 256 + buf * 128 + from, d);
                     tmem_ld_wait32(g);
                     reg_fence32(u);
                     reg_fence32(d);
-                    if (c + 2 > last) release();
+                    if (c == last) release();
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
                         float r[3][2];
@@ -530,11 +536,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                     for (int w = 0; w < 3; ++w) {
                         const uint32_t *v = w == 0 ? g : w == 1 ? u : d;
                         const GemmJob &to = p.job[w];
-                        __syncwarp();
+                        const uint32_t at_place = place + turn * (4 * kGemmStaging);
+                        turn ^= 1u;
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
-                            st_shared_v4(gemm_staged<64>(stage, lane, j), make_uint4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]));
-                        gemm_store_rows<64>(static_cast<__nv_bfloat16 *>(to.out) + row0 * to.ld + col, to.ld * 2, rows, cols * 2, stage, lane);
+                            st_shared_v4(gemm_staged(at_place, lane, group * 4 + j), make_uint4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]));
+                        barrier_sync_64(1 + quarter);
+                        gemm_store_rows<4>(static_cast<__nv_bfloat16 *>(to.out) + row0 * to.ld + col, to.ld * 2, rows, cols * 2, at_place, lane, group * 16);
                     }
                 }
             }
