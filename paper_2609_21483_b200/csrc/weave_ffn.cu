@@ -186,10 +186,10 @@ cudaError_t launch(void (*kernel)(Params...), int grid, int block, size_t smem, 
 // Which kernel takes a call of up to kSmallMaxT tokens: the one whose modelled time is shorter, the products' cost and what
 // else was measured of each.  (us, one launch against pairs of SMs: bf16 2048 x 768: 10.1 / 16.3 with 16 tokens, 16.4 / 16.8
 // with 64, 18.6 / 16.2 with 96; 4096 x 14336: 76 / 92 with 64, 82 / 93 with 96; 8 bits 2048 x 1408: 16.6 / 18.3 with 16,
-// 21.6 / 18.4 with 64; 4096 x 14336: 52 / 58 with 64, 61 / 59 with 128.)
+// 21.6 / 18.4 with 64; 4096 x 14336: 52 / 58 with 64, 61 / 59 with 128.  The pairs' launches take the host some 3 us each.)
 bool small_wins(int T, int products, bool rounds, double small_us, double pairs_us)
 {
-    const double small_rest = 1.0 + products * (rounds ? 6.0 : 3.0) + products * 0.033 * T, pairs_rest = products * (rounds ? 6.5 : 4.0);
+    const double small_rest = 1.0 + products * (rounds ? 6.0 : 3.0) + products * 0.033 * T, pairs_rest = products * (rounds ? 7.0 : 4.0);
     return small_rest + small_us <= pairs_rest + pairs_us;
 }
 double small_us(const Engine &e, int n, bool gated, long long K, int block, int T)
@@ -275,7 +275,7 @@ cudaError_t launch_small(const Engine &e, SmallArgs &a, int T, cudaStream_t stre
 double gemm_tile_us(int ksteps, int accumulator_columns)
 {
     const double bytes = kGemmHalf + accumulator_columns * 64.0, step = bytes / 94000.0 > 0.2 ? bytes / 94000.0 : 0.2;
-    const double epilogue = 0.4 + 0.008 * accumulator_columns;
+    const double epilogue = 0.3 + 0.0055 * accumulator_columns;
     return ksteps * step > epilogue ? ksteps * step : epilogue;
 }
 long long gemm_tiles(int M, int N, int width) { return (long long)((M + 255) / 256) * ((N + width - 1) / width); }
@@ -285,7 +285,7 @@ GemmWidth gemm_width(const Engine &e, int M, int N, int ksteps, int widest, int 
     GemmWidth best = {widest, 1e30};
     for (int w = widest; w * columns >= 64 && w > 0; w -= unit) {
         const long long pairs = e.n_sm / 2, waves = (gemm_tiles(M, N, w) + pairs - 1) / pairs;
-        const double us = waves * gemm_tile_us(ksteps, w * columns) + 0.008 * w * columns;
+        const double us = waves * gemm_tile_us(ksteps, w * columns) + 0.0055 * w * columns;
         if (us < best.us) best = {w, us};
     }
     return best;
@@ -297,7 +297,7 @@ int gemm_width_among(const Engine &e, int M, int N, int ksteps, double others_us
 {
     int best = 256;
     double best_cost = 1e30;
-    for (int w = 256; w >= 64; w -= 64) {
+    for (int w = 256; w >= 128; w /= 2) {        // (copies of an MN-major operand are 64 columns wide in each CTA)
         const long long pairs = e.n_sm / 2, tiles = gemm_tiles(M, N, w), waves = (tiles + pairs - 1) / pairs;
         const double tile = gemm_tile_us(ksteps, w), own = waves * tile, even = (tiles * tile + others_us) / pairs;
         const double cost = own > even ? own : even;

@@ -418,7 +418,7 @@ def test_refusals_on_the_device():
 def test_a_wait_that_gives_up_ends_the_call(int8):
     """One thread block never arrives: every wait behind that barrier expires, the call ends with a status, and the handle
     works again."""
-    T, H, I = 5, 272, 400
+    T, H, I = 5, 1024, 2048          # a shape whose small batches run in one launch, in either form
     x, gate_up, down, _ = block(T, H, I, seed=6)
     if int8:
         ffn = pk.Int8FFN(*pk.quantize_rows(gate_up), *pk.quantize_rows(down), max_tokens=T)
