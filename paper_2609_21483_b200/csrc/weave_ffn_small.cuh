@@ -117,6 +117,12 @@ __device__ __forceinline__ void red_release_add_u64(unsigned long long *p, unsig
 {
     asm volatile("red.release.gpu.global.add.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory");
 }
+__device__ __forceinline__ unsigned long long ld_relaxed_u64(const unsigned long long *p)
+{
+    unsigned long long v;
+    asm volatile("ld.relaxed.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
+    return v;
+}
 __device__ __forceinline__ unsigned long long ld_acquire_u64(const unsigned long long *p)
 {
     unsigned long long v;
@@ -251,25 +257,21 @@ struct SmallBars {
 static_assert(2 * kSmallRed + sizeof(SmallBars) <= kSmallTail, "the tail of shared memory");
 
 // All CTAs' epilogue warps arrive here with what they wrote; true when everybody has.  The counter only grows, by the
-// grid size per barrier and launch, so nothing has to be reset; what it will reach is known to whoever reads it before
-// his own arrival (small_barrier_target).
-__device__ __forceinline__ unsigned long long small_barrier_target(const unsigned long long *counter)
-{
-    const unsigned long long g = gridDim.x;
-    return (ld_acquire_u64(counter) / g + 1) * g;
-}
-__device__ __forceinline__ bool small_grid_barrier(unsigned long long *counter, unsigned long long target, bool ok, bool withheld, const WaitCtx &wc,
+// grid size per barrier and launch, so nothing has to be reset; what it will reach follows from any value of it that was
+// read before the own arrival (`seen`).
+__device__ __forceinline__ bool small_grid_barrier(unsigned long long *counter, unsigned long long seen, bool ok, bool withheld, const WaitCtx &wc,
                                                    int where)
 {
     __threadfence();
     fence_proxy_async_global();          // ordinary stores here, tensor-map loads there
     ok = named_barrier_and<1, 256>(ok);
     if (ok && threadIdx.x == 128) {
+        const unsigned long long g = gridDim.x, target = (seen / g + 1) * g;
         if (!withheld) red_release_add_u64(counter, 1ull);
         unsigned long long t0 = 0;
         unsigned it = 0;
         while (ld_acquire_u64(counter) < target) {
-            __nanosleep(64);             // 148 of these loads at once would keep the last arrivals from the counter
+            __nanosleep(32);             // 148 of these loads at once would keep the last arrivals from the counter
             if ((++it & 31u) == 0u) {
                 if (*reinterpret_cast<volatile int *>(&wc.ctl->status) != 0) { ok = false; break; }
                 const unsigned long long now = globaltimer_ns();
@@ -283,9 +285,7 @@ __device__ __forceinline__ bool small_grid_barrier(unsigned long long *counter, 
         }
         fence_proxy_async_global();
     }
-    ok = named_barrier_and<1, 256>(ok);
-    __threadfence();
-    return ok;
+    return named_barrier_and<1, 256>(ok);
 }
 
 // The epilogue warps round the tokens of a product: one row per CTA, or all rows into this CTA's own copy.
@@ -326,11 +326,27 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
     const WaitCtx wc = {a.ctl, a.timeout_ns};
     constexpr int kBlock = kI8 ? 128 : 64;
 
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kSmallMaxSlots; ++i)
-            for (int j = 0; j < 2; ++j) { mbar_init(&bars.full[j][i], 2); mbar_init(&bars.empty[j][i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&bars.acc_full[i], 1); mbar_init(&bars.acc_empty[i], 8); mbar_init(&bars.tokens[i], 1); }
+    int ahead = 0;           // steps of the first product whose weights are on their way before anything else is set up
+    if (warp == 0) {
+        if (lane < kSmallMaxSlots) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) { mbar_init(&bars.full[j][lane], 2); mbar_init(&bars.empty[j][lane], 1); }
+        } else if (lane < kSmallMaxSlots + 2) {
+            const int i = lane - kSmallMaxSlots;
+            mbar_init(&bars.acc_full[i], 1);
+            mbar_init(&bars.acc_empty[i], 8);
+            mbar_init(&bars.tokens[i], 1);
+        }
         fence_mbar_init();
+        fence_proxy_async_shared();
+        __syncwarp();
+        const SmallShape &s = a.p[0].s;
+        const int col0 = blockIdx.x * s.rounds * s.ct;
+        // (not in front of tokens that every CTA rounds itself: their loads would come behind the weights)
+        if (col0 < s.n && !(kI8 && a.p[0].round_local)) ahead = min(s.slots, s.steps);
+        for (int k = 0; k < ahead; ++k)
+            tma_fill(smem + k * s.slot_bytes, &a.p[0].w, s.kbs == 1 ? k * kBlock : 0, col0, 0, s.kbs == 1 ? 0 : k * s.kbs, &bars.full[0][k],
+                     (uint32_t)s.w_bytes);
     }
     if (warp == 2) { tmem_alloc_one(&bars.tmem_base, (uint32_t)a.tmem_cols); tmem_relinquish_one(); }
     tc_fence_before();
@@ -348,8 +364,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
             const SmallProduct &p = a.p[i];
             const int before = i > 0 ? small_steps(a.p[0].s) : 0, start = i > 0 ? small_first_slot(a.p[0].s, p.s, before) : 0;
             const int turns = i > 0 ? before / a.p[0].s.slots : 0, rest = i > 0 ? before % a.p[0].s.slots : 0;
-            int slot = start, n = 0;
+            int n = i == 0 ? ahead : 0, slot = start + n;
             uint32_t ph = 0;
+            if (i == 0 && slot == p.s.slots) { slot = 0; ph = 1u; }
             if (lane == 0) tma_prefetch_desc(weights ? &p.w : &p.x);
             if (!weights && (i > 0 || (kI8 && p.round_src))) {
                 ok = __all_sync(0xffffffffu, ffn_wait(&bars.tokens[i], 0, wc, 20 + i));
@@ -360,7 +377,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
             for (int r = 0; r < p.s.rounds && ok; ++r) {
                 const int col0 = (blockIdx.x * p.s.rounds + r) * p.s.ct;
                 if (col0 >= p.s.n) break;
-                for (int k = 0; k < p.s.steps; ++k) {
+                for (int k = i == 0 && r == 0 ? ahead : 0; k < p.s.steps; ++k) {
                     bool there = true;
                     if (i == 0 || n >= p.s.slots) {
                         there = ffn_wait(&bars.empty[i][slot], ph ^ 1u, wc, 22 + (int)weights);
@@ -422,17 +439,17 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
         const int acc_row = quarter * 32 + lane;
         uint32_t *const red = reinterpret_cast<uint32_t *>(behind + group * kSmallRed);
         const bool withheld = (int)blockIdx.x == a.withhold;
-        unsigned long long target[3] = {0, 0, 0};
+        unsigned long long seen[3] = {0, 0, 0};
         if (threadIdx.x == 128)
 #pragma unroll
-            for (int j = 0; j < 3; ++j) target[j] = small_barrier_target(&a.ctl->barrier[j]);
+            for (int j = 0; j < 3; ++j) seen[j] = ld_relaxed_u64(&a.ctl->barrier[j]);
         int n = 0;
 #pragma unroll 1        // the second product finds these instructions in the cache
         for (int i = 0; i < a.products && ok; ++i) {
             const SmallProduct &p = a.p[i];
             const SmallShape s = p.s;
             const bool gate = p.gated, out_f32 = p.out_f32;
-            if (i > 0) ok = small_grid_barrier(&a.ctl->barrier[0], target[0], ok, withheld, wc, 26);
+            if (i > 0) ok = small_grid_barrier(&a.ctl->barrier[0], seen[0], ok, withheld, wc, 26);
             if constexpr (kI8) {
                 if (ok && p.round_src) {
                     if (p.round_f32) small_round_rows(static_cast<const float *>(p.round_src), p, a.T, bars.row_max);
@@ -441,7 +458,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
                         fence_proxy_async_global();
                         named_barrier_sync<1, 256>();
                     } else {
-                        ok = small_grid_barrier(&a.ctl->barrier[1 + i], i == 0 ? target[1] : target[2], ok, withheld, wc, 27);
+                        ok = small_grid_barrier(&a.ctl->barrier[1 + i], i == 0 ? seen[1] : seen[2], ok, withheld, wc, 27);
                     }
                 }
             }
