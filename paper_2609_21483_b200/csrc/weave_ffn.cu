@@ -73,7 +73,9 @@ cudaError_t size_gemm()
 template <bool kI8>
 cudaError_t size_small()
 {
-    return cudaFuncSetAttribute(weave_ffn_small_kernel<kI8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmemMax);
+    const cudaError_t err = cudaFuncSetAttribute(weave_ffn_small_kernel<kI8, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmemMax);
+    return err != cudaSuccess ? err
+                              : cudaFuncSetAttribute(weave_ffn_small_kernel<kI8, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmemMax);
 }
 
 int engine_create(Engine &e, void *workspace)
@@ -212,19 +214,24 @@ bool small_product(const Engine &e, SmallArgs &a, int type, const void *w, const
     p.round_src = nullptr;
     p.round_local = copies > 1;
     p.K = K;
-    // with several blocks of K per step they are the maps' last dimension; with one, K is the first, clipped at its end
-    const bool blocks = p.s.kbs > 1;
-    const cuuint64_t row = (cuuint64_t)K * size, inner = blocks ? (cuuint64_t)block : (cuuint64_t)K, count = blocks ? (cuuint64_t)(K / block) : 1;
-    const cuuint64_t wd[4] = {inner, (cuuint64_t)n, gated ? 2u : 1u, count}, ws[3] = {row, row * (cuuint64_t)n, 128};
-    const cuuint32_t wb[4] = {(cuuint32_t)block, (cuuint32_t)p.s.ct, gated ? 2u : 1u, (cuuint32_t)p.s.kbs};
-    const cuuint64_t xd[4] = {inner, (cuuint64_t)T, count, (cuuint64_t)copies}, xs[3] = {row, 128, row * (cuuint64_t)T};
-    const cuuint32_t xb[4] = {(cuuint32_t)block, (cuuint32_t)p.s.box_t, (cuuint32_t)p.s.kbs, 1};
-    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    // with several blocks of K per step they are a dimension of the maps; with one, and behind the last whole block, K is the
+    // first dimension, clipped at its end
     const CUtensorMapDataType dt = size == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-    return e.encode(&p.w, dt, 4, const_cast<void *>(w), wd, ws, wb, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS &&
-           e.encode(&p.x, dt, 4, const_cast<void *>(x), xd, xs, xb, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t row = (cuuint64_t)K * size;
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    const auto maps = [&](CUtensorMap &mw, CUtensorMap &mx, bool blocks) {
+        const cuuint64_t inner = blocks ? (cuuint64_t)block : (cuuint64_t)K, count = blocks ? (cuuint64_t)p.s.full : 1;
+        const cuuint32_t kbs = blocks ? (cuuint32_t)p.s.kbs : 1u;
+        const cuuint64_t wd[4] = {inner, (cuuint64_t)n, gated ? 2u : 1u, count}, ws[3] = {row, row * (cuuint64_t)n, 128};
+        const cuuint32_t wb[4] = {(cuuint32_t)block, (cuuint32_t)p.s.ct, gated ? 2u : 1u, kbs};
+        const cuuint64_t xd[4] = {inner, (cuuint64_t)T, count, (cuuint64_t)copies}, xs[3] = {row, 128, row * (cuuint64_t)T};
+        const cuuint32_t xb[4] = {(cuuint32_t)block, (cuuint32_t)p.s.box_t, kbs, 1};
+        return e.encode(&mw, dt, 4, const_cast<void *>(w), wd, ws, wb, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS &&
+               e.encode(&mx, dt, 4, const_cast<void *>(x), xd, xs, xb, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    return maps(p.w, p.x, p.s.kbs > 1) && (p.s.tail_at < 0 || maps(p.w_tail, p.x_tail, false));
 }
 // Up to two tokens every CTA rounds for itself, 1.4 us each; from three on one row per CTA and a grid barrier behind them
 // (3 to 4 us while the ring fills) take less.
@@ -261,12 +268,15 @@ cudaError_t launch_small(const Engine &e, SmallArgs &a, int T, cudaStream_t stre
     a.withhold = e.withhold;
     a.T = T;
     a.acc_cols = 0;
+    bool tail = false;
     for (int i = 0; i < a.products; ++i) {
+        tail = tail || a.p[i].s.tail_at >= 0;
         const int cols = a.p[i].s.kbs * a.p[i].s.box_t;
         a.acc_cols = cols > a.acc_cols ? cols : a.acc_cols;
     }
     for (a.tmem_cols = 32; a.tmem_cols < 2 * a.acc_cols;) a.tmem_cols *= 2;
-    return launch(weave_ffn_small_kernel<kI8>, e.n_sm, kSmallThreads, kSmallSmemMax, kCooperative, stream, a);
+    return launch(tail ? weave_ffn_small_kernel<kI8, true> : weave_ffn_small_kernel<kI8, false>, e.n_sm, kSmallThreads, kSmallSmemMax, kCooperative,
+                  stream, a);
 }
 
 // Columns of a tile (a multiple of `unit`; each takes `columns` of the accumulator's): as narrow as the number of waves

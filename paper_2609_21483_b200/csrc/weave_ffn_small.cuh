@@ -10,7 +10,8 @@
 // rows and columns are used, so where a CTA has few rows, `kbs` blocks of K lie side by side: A = (block, row) on M,
 // B = (block, token) on N, of D only the blocks on the diagonal are used, and the epilogue adds them up.  With 28 rows
 // and 16 tokens that is 4 blocks per product, 5.6 us of tensor pipe for K = 14336 instead of 23.6.  One tensor copy
-// brings all blocks of a step: they are a dimension of the tensor map (where K is whole blocks; else kbs = 1).
+// brings all blocks of a step: they are a dimension of the tensor map.  What K has behind its last whole block is a step
+// of its own, clipped by another map, whose product is the block's own N wide.
 //
 // Order.  Weights are fetched as fast as slots of the ring become free, straight from the first product into the
 // second; tokens follow when they are there.  The result h of the first product crosses between SMs through L2 behind a
@@ -149,14 +150,17 @@ struct SmallShape {
     int rows;            // weight rows per block of K: ct, gated 2 ct
     int kbs;             // blocks of K per step
     int steps;           // steps of a tile
+    int full;            // whole blocks of K
+    int tail_at;         // kbs > 1: the step of what is left behind them, or -1
     int box_t;           // tokens of a block, padded
     int w_bytes, x_bytes;
     int slots, slot_bytes, x_offset;     // of the ring while this product runs
 };
 
-__host__ __device__ inline int small_box(int T, int kbs)
+// N = kbs * box is a multiple of 16, and so is the box where a tail's product is one box wide
+__host__ __device__ inline int small_box(int T, int kbs, bool tail)
 {
-    return kbs == 1 ? (T + 15) & ~15 : (T + 7) & ~7;          // N = kbs * box is a multiple of 16
+    return kbs == 1 || tail ? (T + 15) & ~15 : (T + 7) & ~7;
 }
 
 // The ring's slots have another size in the second product.  Its first one is the first that starts behind the slot the
@@ -183,9 +187,11 @@ inline SmallShape small_shape(int n, bool gated, long long K, int block, int T, 
     s.ct = (int)((n + (long long)ctas * s.rounds - 1) / ((long long)ctas * s.rounds));
     s.rows = gated ? 2 * s.ct : s.ct;
     s.kbs = kbs;
-    s.box_t = small_box(T, kbs);
-    const long long blocks = (K + block - 1) / block;
-    s.steps = (int)((blocks + kbs - 1) / kbs);
+    s.full = (int)(K / block);
+    const bool tail = kbs > 1 && K % block != 0;
+    s.box_t = small_box(T, kbs, tail);
+    s.steps = kbs > 1 ? (s.full + kbs - 1) / kbs + tail : (int)((K + block - 1) / block);
+    s.tail_at = tail ? s.steps - 1 : -1;
     s.w_bytes = kbs * s.rows * 128;
     s.x_bytes = kbs * s.box_t * 128;
     s.x_offset = (s.w_bytes + 1023) & ~1023;
@@ -196,25 +202,25 @@ inline SmallShape small_shape(int n, bool gated, long long K, int block, int T, 
 }
 // Microseconds that a product takes with this plan, from measurements: the chip reads weights at 6.4 TB/s (a little less
 // where a step takes only 128 or 256 bytes of each row), an SM takes in 90 bytes per ns, weights and tokens, a step of the
-// ring is 250 ns at least, a tile's epilogue holds up the next one by some 0.15 us.  (16 tokens, 4096 -> 2 x 14336 -> 4096,
-// us for 1, 2, 4, 8 blocks per step in both products: 99, 72, 59.5, 63; 64 tokens with 1, 2, 4 in the first and 4 in the
-// second: 74, 78, 90; one token through 2048 x 768: 17.2, 12.6, 9.8, 9.6.)
+// ring is 250 ns at least, a tile's epilogue holds up the next one by some 0.15 us, a tail's own maps cost 1 us.  (16
+// tokens, 4096 -> 2 x 14336 -> 4096, us for 1, 2, 4, 8 blocks per step in both products: 99, 72, 59.5, 63; 64 tokens with
+// 1, 2, 4 in the first and 4 in the second: 74, 78, 90; one token through 2048 x 768: 17.2, 12.6, 9.8, 9.6; 1672 x 12720
+// with one block per step and with more and a tail: 58, 31.)
 inline double small_cost(const SmallShape &s, long long K, int block, int T)
 {
     const double weights = (double)s.n * (s.rows / s.ct) * ((double)K / block * 128.0);
     const double chip = weights / (s.kbs == 1 ? 5900.0 : s.kbs == 2 ? 6100.0 : 6400.0);
     const double steps = (double)s.rounds * s.steps;
     const double sm = steps * (s.w_bytes + s.kbs * T * 128.0) / 90.0, issue = steps * 250.0;
-    return ((chip > sm ? chip : sm) > issue ? (chip > sm ? chip : sm) : issue) / 1000.0 + 0.15 * s.rounds;
+    return ((chip > sm ? chip : sm) > issue ? (chip > sm ? chip : sm) : issue) / 1000.0 + 0.15 * s.rounds + (s.tail_at >= 0 ? 1.0 : 0.0);
 }
 inline SmallShape small_plan(int n, bool gated, long long K, int block, int T, int ctas)
 {
     SmallShape best = small_shape(n, gated, K, block, T, ctas, 1);
-    if (K % block == 0)          // the maps of several blocks cannot clip the last one
-        for (int kbs = 2; kbs <= 8 && kbs <= K / block && kbs * small_box(T, kbs) <= 256; kbs *= 2) {
-            const SmallShape s = small_shape(n, gated, K, block, T, ctas, kbs);
-            if (small_cost(s, K, block, T) < small_cost(best, K, block, T)) best = s;
-        }
+    for (int kbs = 2; kbs <= 8 && kbs <= K / block && kbs * small_box(T, kbs, K % block != 0) <= 256; kbs *= 2) {
+        const SmallShape s = small_shape(n, gated, K, block, T, ctas, kbs);
+        if (small_cost(s, K, block, T) < small_cost(best, K, block, T)) best = s;
+    }
     return best;
 }
 
@@ -223,6 +229,7 @@ inline SmallShape small_plan(int n, bool gated, long long K, int block, int T, i
 struct alignas(64) SmallProduct {
     CUtensorMap w;           // {K, rows, halves, 1} or {block, rows, halves, blocks}
     CUtensorMap x;           // {K, T, 1, copies} or {block, T, blocks, copies}
+    CUtensorMap w_tail, x_tail;      // with a tail: the first forms
     SmallShape s;
     int gated, out_f32;
     const float *row_scale;  // 8-bit forms: [T], and [n] (gated: [2n], gate then up)
@@ -300,6 +307,22 @@ __device__ __noinline__ void small_round_rows(const X *src, const SmallProduct &
     }
 }
 
+// a step's copies
+template <bool kTail>
+__device__ __forceinline__ void small_fill_weights(const SmallProduct &p, int k, int tail_at, int block, int col0, uint32_t dst, uint64_t *full)
+{
+    const SmallShape &s = p.s;
+    if (kTail && k == tail_at) tma_fill(dst, &p.w_tail, s.full * block, col0, 0, 0, full, (uint32_t)(s.rows * 128));
+    else tma_fill(dst, &p.w, s.kbs == 1 ? k * block : 0, col0, 0, s.kbs == 1 ? 0 : k * s.kbs, full, (uint32_t)s.w_bytes);
+}
+template <bool kTail>
+__device__ __forceinline__ void small_fill_tokens(const SmallProduct &p, int k, int tail_at, int block, int copy, uint32_t dst, uint64_t *full)
+{
+    const SmallShape &s = p.s;
+    if (kTail && k == tail_at) tma_fill(dst, &p.x_tail, s.full * block, 0, 0, copy, full, (uint32_t)(s.box_t * 128));
+    else tma_fill(dst, &p.x, s.kbs == 1 ? k * block : 0, 0, s.kbs == 1 ? 0 : k * s.kbs, copy, full, (uint32_t)s.x_bytes);
+}
+
 template <bool kI8>
 __device__ __forceinline__ float small_value(uint32_t acc, float sx, float sw)
 {
@@ -315,7 +338,8 @@ __device__ __forceinline__ uint4 small_add(uint4 a, uint4 b)
                           __float_as_uint(__uint_as_float(a.z) + __uint_as_float(b.z)), __float_as_uint(__uint_as_float(a.w) + __uint_as_float(b.w)));
 }
 
-template <bool kI8>
+// kTail: one of the products has a tail
+template <bool kI8, bool kTail>
 __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const __grid_constant__ SmallArgs a)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -344,9 +368,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
         const int col0 = blockIdx.x * s.rounds * s.ct;
         // (not in front of tokens that every CTA rounds itself: their loads would come behind the weights)
         if (col0 < s.n && !(kI8 && a.p[0].round_local)) ahead = min(s.slots, s.steps);
-        for (int k = 0; k < ahead; ++k)
-            tma_fill(smem + k * s.slot_bytes, &a.p[0].w, s.kbs == 1 ? k * kBlock : 0, col0, 0, s.kbs == 1 ? 0 : k * s.kbs, &bars.full[0][k],
-                     (uint32_t)s.w_bytes);
+        for (int k = 0; k < ahead; ++k) small_fill_weights<kTail>(a.p[0], k, s.tail_at, kBlock, col0, smem + k * s.slot_bytes, &bars.full[0][k]);
     }
     if (warp == 2) { tmem_alloc_one(&bars.tmem_base, (uint32_t)a.tmem_cols); tmem_relinquish_one(); }
     tc_fence_before();
@@ -372,8 +394,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
                 ok = __all_sync(0xffffffffu, ffn_wait(&bars.tokens[i], 0, wc, 20 + i));
                 fence_proxy_async_global();
             }
-            const bool one = p.s.kbs == 1;
-            const int copy = p.round_local ? (int)blockIdx.x : 0;
+            const int copy = p.round_local ? (int)blockIdx.x : 0, tail_at = p.s.tail_at;
             for (int r = 0; r < p.s.rounds && ok; ++r) {
                 const int col0 = (blockIdx.x * p.s.rounds + r) * p.s.ct;
                 if (col0 >= p.s.n) break;
@@ -394,8 +415,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
                     if (!ok) break;
                     uint64_t *full = &bars.full[i][slot];
                     const uint32_t dst = smem + slot * p.s.slot_bytes;
-                    if (weights) tma_fill(dst, &p.w, one ? k * kBlock : 0, col0, 0, one ? 0 : k * p.s.kbs, full, (uint32_t)p.s.w_bytes);
-                    else tma_fill(dst + p.s.x_offset, &p.x, one ? k * kBlock : 0, 0, one ? 0 : k * p.s.kbs, copy, full, (uint32_t)p.s.x_bytes);
+                    if (weights) small_fill_weights<kTail>(p, k, tail_at, kBlock, col0, dst, full);
+                    else small_fill_tokens<kTail>(p, k, tail_at, kBlock, copy, dst + p.s.x_offset, full);
                     ++n;
                     if (++slot == p.s.slots) slot = 0;
                     if (slot == start) ph ^= 1u;
@@ -413,6 +434,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
             int slot = start;
             uint32_t ph = 0;
             const uint32_t idesc = kI8 ? umma_idesc_i8(128, s.kbs * s.box_t) : umma_idesc_bf16(128, s.kbs * s.box_t);
+            const int tail_at = s.tail_at;
+            // the first block's columns alone: what lies in the other blocks' places is not this step's
+            const uint32_t idesc_tail = kI8 ? umma_idesc_i8(128, s.box_t) : umma_idesc_bf16(128, s.box_t);
             for (int r = 0; r < s.rounds && ok; ++r, ++n) {
                 if ((blockIdx.x * s.rounds + r) * s.ct >= s.n) break;
                 const int buf = n & 1;
@@ -423,7 +447,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) weave_ffn_small_kernel(const
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t w = smem + slot * s.slot_bytes;
-                    ffn_mma_kstep_one<kI8>(tmem + (uint32_t)(buf * a.acc_cols), umma_desc_sw128(w), umma_desc_sw128(w + s.x_offset), idesc,
+                    ffn_mma_kstep_one<kI8>(tmem + (uint32_t)(buf * a.acc_cols), umma_desc_sw128(w), umma_desc_sw128(w + s.x_offset),
+                                           kTail && k == tail_at ? idesc_tail : idesc,
                                            (uint32_t)(k != 0), &bars.empty[i][slot]);
                     if (++slot == s.slots) slot = 0;
                     if (slot == start) ph ^= 1u;
