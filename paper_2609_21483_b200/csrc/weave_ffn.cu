@@ -30,6 +30,7 @@ size_t up1024(size_t n) { return (n + 1023) & ~(size_t)1023; }
 struct Engine {
     int device, n_sm;
     FfnCtl *ctl;
+    uint32_t *partials;        // kGemmSplitBytes; null where no call splits K
     unsigned long long timeout_ns;
     cudaStream_t last_stream;
     int last_cuda_error;
@@ -67,7 +68,11 @@ bool outputs_clear(const Range *out, int n_out, const Range *in, int n_in)
 template <int kEpi, bool kI8>
 cudaError_t size_gemm()
 {
-    return cudaFuncSetAttribute(weave_gemm_kernel<kEpi, kI8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmemBytes);
+    if constexpr (kEpi == kEpiStore || kEpi == kEpiScaled) {
+        const cudaError_t err = cudaFuncSetAttribute(weave_gemm_kernel<kEpi, kI8, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmemBytes);
+        if (err != cudaSuccess) return err;
+    }
+    return cudaFuncSetAttribute(weave_gemm_kernel<kEpi, kI8, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmemBytes);
 }
 
 template <bool kI8>
@@ -282,6 +287,7 @@ cudaError_t launch_small(const Engine &e, SmallArgs &a, int T, cudaStream_t stre
 // Columns of a tile (a multiple of `unit`; each takes `columns` of the accumulator's): as narrow as the number of waves
 // over the pairs of SMs allows, and rather more waves of narrower tiles than idle pairs.  A k-step takes the time of its
 // bytes into an SM (94 per ns: 0.35 us for 32 KB), 0.2 us at least; a tile's epilogue is hidden but for the last one's.
+constexpr int kSplitMinT = 32;
 double gemm_tile_us(int ksteps, int accumulator_columns)
 {
     const double bytes = kGemmHalf + accumulator_columns * 64.0, step = bytes / 94000.0 > 0.2 ? bytes / 94000.0 : 0.2;
@@ -289,31 +295,53 @@ double gemm_tile_us(int ksteps, int accumulator_columns)
     return ksteps * step > epilogue ? ksteps * step : epilogue;
 }
 long long gemm_tiles(int M, int N, int width) { return (long long)((M + 255) / 256) * ((N + width - 1) / width); }
-struct GemmWidth { int width; double us; };
-GemmWidth gemm_width(const Engine &e, int M, int N, int ksteps, int widest, int unit, int columns)
+// K is split over pairs where tiles are few and K is long: parts of at least eight steps, all of them in one wave.  (us
+// whole / split: T = 128, 1016 x 14840: 62.5 / 38.4; T = 270: 72.1 / 49.5; 4096 x 14336: T = 128 92.7 / 82.1, T = 200 96.6 /
+// 86.3; gradient T = 596, 264 x 8120: 71.9 / 47.1; 8 bits T = 257, 14336 -> 520: 28.4 / 19.1.)  Whoever adds the parts up
+// needs a few round trips and reads them all.
+double gemm_join_us(int splits, int width) { return 3.0 + splits * width * 512 / 60000.0; }
+int gemm_splits(const Engine &e, long long tiles, int ksteps, int width)        // at most
 {
-    GemmWidth best = {widest, 1e30};
+    if (width > kGemmSplitWidth || !e.partials) return 1;
+    const long long units = e.n_sm / 2 < kGemmSplitUnits ? e.n_sm / 2 : kGemmSplitUnits, s = units / tiles < ksteps / 8 ? units / tiles : ksteps / 8;
+    return s < 1 ? 1 : (int)s;
+}
+// Workspace for it.  Up to 32 tokens the small batches' kernel leaves nothing to gain (within 1 % there), so that a handle for
+// them, of which a model may have hundreds, stays small.
+size_t gemm_split_room(int N, int ksteps, int max_tokens, bool backward)
+{
+    const bool some = (max_tokens > kSplitMinT || backward) && ksteps >= 16 && 2 * ((N + kGemmSplitWidth - 1) / kGemmSplitWidth) <= kGemmSplitUnits;
+    return some ? kGemmSplitBytes : 0;
+}
+struct GemmWidth { int width, splits; double us; };
+GemmWidth gemm_width(const Engine &e, int M, int N, int ksteps, int widest, int unit, int columns, bool may_split)
+{
+    GemmWidth best = {widest, 1, 1e30};
     for (int w = widest; w * columns >= 64 && w > 0; w -= unit) {
-        const long long pairs = e.n_sm / 2, waves = (gemm_tiles(M, N, w) + pairs - 1) / pairs;
-        const double us = waves * gemm_tile_us(ksteps, w * columns) + 0.0055 * w * columns;
-        if (us < best.us) best = {w, us};
+        const long long tiles = gemm_tiles(M, N, w), pairs = e.n_sm / 2, waves = (tiles + pairs - 1) / pairs;
+        const double end = 0.0055 * w * columns, us = waves * gemm_tile_us(ksteps, w * columns) + end;
+        if (us < best.us) best = {w, 1, us};
+        for (int s = may_split ? gemm_splits(e, tiles, ksteps, w) : 1; s > 1; --s) {
+            const double split_us = gemm_tile_us((ksteps + s - 1) / s, w) + end + gemm_join_us(s, w);
+            if (split_us < best.us) best = {w, s, split_us};
+        }
     }
     return best;
 }
 // ... of the long product in a launch with others, which fill the pairs that it leaves: the longer of its own waves and
 // of all work spread evenly.  (Whole gradient, us with 256, 192, 128, 64 columns of dx in a tile: T = 257, 2048 x 1408: 35.5,
-// 32.1, 30.7, 34.6; T = 777, 1096 x 2744: 66.5, 66.1, 67.0, 74.4.)
-int gemm_width_among(const Engine &e, int M, int N, int ksteps, double others_us)
+// 32.1, 30.7, 34.6; T = 777, 1096 x 2744: 66.5, 66.1, 67.0, 74.4.)  A join holds up the tiles behind it, too.
+GemmWidth gemm_width_among(const Engine &e, int M, int N, int ksteps, double others_us)
 {
-    int best = 256;
-    double best_cost = 1e30;
+    GemmWidth best = {256, 1, 1e30};
+    const long long pairs = e.n_sm / 2;
     for (int w = 256; w >= 128; w /= 2) {        // (copies of an MN-major operand are 64 columns wide in each CTA)
-        const long long pairs = e.n_sm / 2, tiles = gemm_tiles(M, N, w), waves = (tiles + pairs - 1) / pairs;
-        const double tile = gemm_tile_us(ksteps, w), own = waves * tile, even = (tiles * tile + others_us) / pairs;
-        const double cost = own > even ? own : even;
-        if (cost < best_cost) {
-            best_cost = cost;
-            best = w;
+        const long long tiles = gemm_tiles(M, N, w);
+        for (int s = gemm_splits(e, tiles, ksteps, w); s > 0; --s) {
+            const long long waves = (tiles * s + pairs - 1) / pairs;
+            const double tile = gemm_tile_us((ksteps + s - 1) / s, w), even = (tiles * s * tile + others_us) / pairs;
+            const double us = (waves * tile > even ? waves * tile : even) + (s > 1 ? 4.0 + gemm_join_us(s, w) : 0.0);
+            if (us < best.us) best = {w, s, us};
         }
     }
     return best;
@@ -326,9 +354,10 @@ int gemm_rows(int M)
     return (((M + 2 * tiles - 1) / (2 * tiles)) + 7) & ~7;
 }
 
-void gemm_job(GemmJob &j, int M, int N, long long K, int step, int width, bool a_mn, bool b_mn, void *out, long long ld)
+void gemm_job(GemmJob &j, int M, int N, long long K, int step, int width, bool a_mn, bool b_mn, void *out, long long ld, int splits = 1)
 {
     j.M = M;
+    j.splits = splits;
     j.N = N;
     j.ksteps = (int)((K + step - 1) / step);
     j.a_mn = a_mn;
@@ -348,6 +377,7 @@ cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int jobs, int b_bytes, Lau
 {
     a.ctl = e.ctl;
     a.timeout_ns = e.timeout_ns;
+    a.partials = e.partials;
     a.a_bytes = 0;
     for (int i = 0; i < jobs; ++i) a.a_bytes = a.job[i].rows * 128 > a.a_bytes ? a.job[i].rows * 128 : a.a_bytes;
     a.stage_bytes = a.a_bytes + b_bytes;
@@ -355,14 +385,19 @@ cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int jobs, int b_bytes, Lau
     if (a.stages > kGemmMaxStages) a.stages = kGemmMaxStages;
     const long long pairs = e.n_sm / 2;
     long long tiles = 0;
-    for (int i = 0; i < jobs; ++i) tiles += (long long)a.job[i].tiles_m * a.job[i].tiles_n;
+    for (int i = 0; i < jobs; ++i) tiles += (long long)a.job[i].tiles_m * a.job[i].tiles_n * a.job[i].splits;
     const int used = (int)(tiles < pairs ? tiles : pairs);
     a.extra = 0;
     if (kEpi == kEpiStore) {
-        for (int i = jobs; i < 3; ++i) a.job[i].tiles_m = a.job[i].tiles_n = 0;
-        if (jobs > 1) a.extra = (int)(gemm_tile_us(a.job[0].ksteps, a.job[0].width) / gemm_tile_us(a.job[1].ksteps, a.job[1].width) + 0.5);
+        for (int i = jobs; i < 3; ++i) {
+            a.job[i].tiles_m = a.job[i].tiles_n = 0;
+            a.job[i].splits = 1;
+        }
+        if (jobs > 1) a.extra = (int)(gemm_tile_us(a.job[0].ksteps / a.job[0].splits, a.job[0].width) / gemm_tile_us(a.job[1].ksteps, a.job[1].width) + 0.5);
     }
-    return launch(weave_gemm_kernel<kEpi, kI8>, used * 2, kGemmThreads, kGemmSmemBytes, kind, stream, a);
+    if constexpr (kEpi == kEpiStore || kEpi == kEpiScaled)
+        if (a.job[0].splits > 1) return launch(weave_gemm_kernel<kEpi, kI8, true>, used * 2, kGemmThreads, kGemmSmemBytes, kind, stream, a);
+    return launch(weave_gemm_kernel<kEpi, kI8, false>, used * 2, kGemmThreads, kGemmSmemBytes, kind, stream, a);
 }
 
 template <class X, int kThreads>
@@ -393,7 +428,7 @@ cudaError_t launch_quant(const void *x, int type, int rows, int cols, int8_t *q,
 
 namespace {
 struct FfnLayout {
-    size_t h, dgu, xq, x_scale, hq, h_scale, control, total;
+    size_t partials, partial_bytes, h, dgu, xq, x_scale, hq, h_scale, control, total;
 };
 bool ffn_shape_ok(const weave_ffn_config *c)
 {
@@ -412,6 +447,10 @@ FfnLayout ffn_layout(const weave_ffn_config *c)
     const size_t T = (size_t)c->max_tokens, I = (size_t)c->ffn;
     size_t at = up1024(sizeof(FfnCtl));
     L.control = at;
+    L.partials = at;
+    const int step = c->weight_type == WEAVE_INT8 ? 128 : 64;
+    L.partial_bytes = gemm_split_room(c->hidden, (c->ffn * (c->backward ? 2 : 1) + step - 1) / step, c->max_tokens, c->backward);
+    at += L.partial_bytes;
     L.h = at;
     at += up1024(T * (size_t)line_pitch(c->ffn) * 2);
     if (c->backward) {
@@ -464,6 +503,7 @@ int weave_ffn_create(const weave_ffn_config *cfg, weave_ffn_t *out)
     h->L = L;
     h->ws = static_cast<uint8_t *>(cfg->workspace);
     int rc = engine_create(h->e, cfg->workspace);
+    h->e.partials = L.partial_bytes ? reinterpret_cast<uint32_t *>(h->ws + L.partials) : nullptr;
     if (rc == WEAVE_OK) rc = engine_clear(h->e, L.control);
     if (rc != WEAVE_OK) {
         delete h;
@@ -493,7 +533,8 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     const void *left = i8 ? static_cast<const void *>(xq) : x, *mid = i8 ? static_cast<const void *>(hq) : hbuf;
     cudaError_t err = cudaSuccess;
     const int step = i8 ? 128 : 64;
-    const GemmWidth up_w = gemm_width(h->e, T, I, (H + step - 1) / step, 128, 8, 2), down_w = gemm_width(h->e, T, H, (I + step - 1) / step, 256, 16, 1);
+    const GemmWidth up_w = gemm_width(h->e, T, I, (H + step - 1) / step, 128, 8, 2, false);
+    const GemmWidth down_w = gemm_width(h->e, T, H, (I + step - 1) / step, 256, 16, 1, T > kSplitMinT);
     if (T <= kSmallMaxT && small_wins(T, 2, i8, small_us(h->e, I, true, H, step, T) + small_us(h->e, H, false, I, step, T), up_w.us + down_w.us)) {
         SmallArgs a;
         a.products = 0;
@@ -517,7 +558,7 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
         !map_k(h->e, d.job[0].b[0], type, h->cfg.down, H, I, wide_d / 2))
         return WEAVE_ERR_CUDA;
     gemm_job(g.job[0], T, I, H, step, wide, false, false, hbuf, pitch);
-    gemm_job(d.job[0], T, H, I, step, wide_d, false, false, out, H);
+    gemm_job(d.job[0], T, H, I, step, wide_d, false, false, out, H, down_w.splits);
     g.row_scale = xs;
     g.col_scale = h->cfg.gate_up_scale;
     d.job[0].b[1] = d.job[0].b[0];
@@ -557,7 +598,7 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     uint8_t *hbuf = h->ws + h->L.h, *dgu = h->ws + h->L.dgu;
     // h and [dg du] from x and dy
     GemmArgs g;
-    const int wide = gemm_width(h->e, T, I, (H + 63) / 64 * 3 / 2, 128, 64, 2).width;
+    const int wide = gemm_width(h->e, T, I, (H + 63) / 64 * 3 / 2, 128, 64, 2, false).width;
     const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * 2;
     const int rows_a = gemm_rows(T);
     const long long h_pitch = line_pitch(I), dgu_pitch = line_pitch(2ll * I);
@@ -580,7 +621,8 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     if (!ok) return WEAVE_ERR_CUDA;
     for (int i = 0; i < 3; ++i) d.job[i].b[1] = d.job[i].b[0];
     const double others = (gemm_tiles(2 * I, H, 256) + gemm_tiles(H, I, 256)) * gemm_tile_us((T + 63) / 64, 256);
-    gemm_job(d.job[0], T, H, 2ll * I, 64, gemm_width_among(h->e, T, H, (2 * I + 63) / 64, others), false, true, dx, H);
+    const GemmWidth dx_w = gemm_width_among(h->e, T, H, (2 * I + 63) / 64, others);
+    gemm_job(d.job[0], T, H, 2ll * I, 64, dx_w.width, false, true, dx, H, dx_w.splits);
     gemm_job(d.job[1], 2 * I, H, T, 64, 256, true, true, dgate_up, H);
     gemm_job(d.job[2], H, I, T, 64, 256, true, true, ddown, I);
     err = launch_gemm<kEpiStore, false>(h->e, d, 3, kGemmHalf, kBehind, stream);
@@ -616,7 +658,7 @@ int weave_ffn_destroy(weave_ffn_t h)
 // ------------------------------------------------------------------------------------ 8-bit integers
 
 namespace {
-struct Int8Layout { size_t xq, x_scale, control, total; };
+struct Int8Layout { size_t partials, partial_bytes, xq, x_scale, control, total; };
 bool int8_shape_ok(const weave_int8_linear_config *c)
 {
     return c && c->in_features > 0 && c->in_features % 16 == 0 && c->in_features <= kMaxWidth && c->out_features > 0 &&
@@ -627,6 +669,9 @@ Int8Layout int8_layout(const weave_int8_linear_config *c)
     Int8Layout L;
     size_t at = up1024(sizeof(FfnCtl));
     L.control = at;
+    L.partials = at;
+    L.partial_bytes = gemm_split_room(c->out_features, (c->in_features + 127) / 128, c->max_tokens, false);
+    at += L.partial_bytes;
     L.xq = at;
     at += up1024(small_round_bytes(c->max_tokens, c->in_features));
     L.x_scale = at;
@@ -678,6 +723,7 @@ int weave_int8_linear_create(const weave_int8_linear_config *cfg, weave_int8_lin
     h->L = L;
     h->ws = static_cast<uint8_t *>(cfg->workspace);
     int rc = engine_create(h->e, cfg->workspace);
+    h->e.partials = L.partial_bytes ? reinterpret_cast<uint32_t *>(h->ws + L.partials) : nullptr;
     if (rc == WEAVE_OK) rc = engine_clear(h->e, L.control);
     if (rc != WEAVE_OK) {
         delete h;
@@ -710,7 +756,7 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     const void *q = round ? xq : x;
     if (round) x_scale = xs;
     const bool direct = (size_t)N * out_size % 16 != 0;
-    const GemmWidth w = gemm_width(h->e, T, N, (K + 127) / 128, 256, 16, 1);
+    const GemmWidth w = gemm_width(h->e, T, N, (K + 127) / 128, 256, 16, 1, T > kSplitMinT);
     if (T <= kSmallMaxT && small_wins(T, 1, round, small_us(h->e, N, false, K, 128, T), w.us)) {
         SmallArgs a;
         a.products = 0;
@@ -734,7 +780,7 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     g.col_scale = h->cfg.scale;
     if (!map_k(h->e, g.job[0].a, WEAVE_INT8, q, T, K, rows_a) || !map_k(h->e, g.job[0].b[0], WEAVE_INT8, h->cfg.weight, N, K, wide / 2)) return WEAVE_ERR_CUDA;
     g.job[0].b[1] = g.job[0].b[0];
-    gemm_job(g.job[0], T, N, K, 128, wide, false, false, out, N);
+    gemm_job(g.job[0], T, N, K, 128, wide, false, false, out, N, w.splits);
     err = launch_gemm<kEpiScaled, true>(h->e, g, 1, wide * 64, round ? kBehind : kPlain, stream);
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
 }

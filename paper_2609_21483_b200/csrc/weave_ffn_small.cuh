@@ -99,21 +99,6 @@ __device__ __forceinline__ void tmem_ld_wait8(uint32_t (&r)[8])
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
                  :: "memory");
 }
-// a barrier of some of the CTA's warps that also says whether all of their threads brought `true`
-template <int ID, int THREADS>
-__device__ __forceinline__ bool named_barrier_and(bool mine)
-{
-    uint32_t all;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.u32 p, %1, 0;\n\t"
-        "bar.red.and.pred q, %2, %3, p;\n\t"
-        "selp.u32 %0, 1, 0, q;\n\t}"
-        : "=r"(all)
-        : "r"((uint32_t)mine), "n"(ID), "n"(THREADS)
-        : "memory");
-    return all != 0;
-}
 __device__ __forceinline__ void red_release_add_u64(unsigned long long *p, unsigned long long v)
 {
     asm volatile("red.release.gpu.global.add.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory");

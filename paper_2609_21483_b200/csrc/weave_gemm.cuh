@@ -10,8 +10,11 @@
 //   kEpiScaledGated h as above from scaled g and u (128)                                 8-bit integers, K-major
 //
 // A tile is 256 rows of A (128 per CTA) by up to 256 accumulator columns (fewer where that fills the last wave).  A k-step
-// is 128 bytes of K (64 bf16 or 128 8-bit integers): up to 16 KB of A and of B per CTA, 192 KB of them in flight.  Rows, columns and K that stick out over
-// the matrices are zero-filled by the tensor maps on the way in and clipped by them on the way out.
+// is 128 bytes of K (64 bf16 or 128 8-bit integers): up to 16 KB of A and of B per CTA, 192 KB of them in flight.  Rows,
+// columns and K that stick out over the matrices are zero-filled by the tensor maps on the way in and clipped on the way out.
+//
+// Where tiles are few and K is long, K is cut into parts for different pairs (kSplit): each part's sums go to the workspace,
+// and the last to arrive at a tile, which waits for nobody, adds them up in the order of K: the same bits every time.
 //
 // Bound: the tensor pipe (256 x 256 x 16 takes 128 cycles) and, over more than some milliseconds, the power limit.
 #pragma once
@@ -28,8 +31,12 @@ struct FfnCtl {
     int where;           // which wait that was
     unsigned pad[30];
     unsigned long long barrier[16];      // grid barriers of the small batches' kernel: arrivals since creation
+    unsigned arrived[192];               // products whose K is split: arrivals per tile and CTA of a pair, zero between launches
 };
-static_assert(sizeof(FfnCtl) == 256, "the workspace layout counts on it");
+static_assert(sizeof(FfnCtl) == 1024, "the workspace layout counts on it");
+constexpr int kGemmSplitUnits = 74;      // tiles times parts of K, at most, and
+constexpr int kGemmSplitWidth = 128;     // columns of such a tile
+constexpr size_t kGemmSplitBytes = (size_t)kGemmSplitUnits * 2 * kGemmSplitWidth * 128 * 4;
 
 constexpr int kFfnErrTimeout = -6;      // WEAVE_ERR_TIMEOUT
 
@@ -120,6 +127,22 @@ __device__ __forceinline__ void ffn_mma_kstep_pair(uint32_t d_tmem, uint64_t a_d
 #undef WEAVE_KSTEP_PAIR
 }
 
+// a barrier of some of the CTA's warps that also says whether all of their threads brought `true`
+template <int ID, int THREADS>
+__device__ __forceinline__ bool named_barrier_and(bool mine)
+{
+    uint32_t all;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "bar.red.and.pred q, %2, %3, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(all)
+        : "r"((uint32_t)mine), "n"(ID), "n"(THREADS)
+        : "memory");
+    return all != 0;
+}
+
 // ------------------------------------------------------------------------------------ the activation
 
 // s = sigmoid(g).  exp overflows to inf for g below -88, where s is 0 either way; NaN and +inf come through.
@@ -145,11 +168,14 @@ struct alignas(64) GemmJob {
                              // 64 where B is MN-major (kEpiGrad, too): with 16 of them in a CTA
                              // the products came out wrong, with 32 right
     int tiles_m, tiles_n, group_m;
+    int splits;              // parts of K that are worked on by different pairs (kEpiStore's job 0, kEpiScaled; else 1): fp32 or
+                             // int32 sums in `partials`, added up in the order of K by whoever arrives last
 };
 
 struct alignas(64) GemmArgs {
     GemmJob job[3];
     FfnCtl *ctl;
+    uint32_t *partials;      // [tile][part][CTA of the pair][column][128]
     unsigned long long timeout_ns;
     const float *row_scale;  // scaled forms: [M] and [N] (gated: [2N], gate then up)
     const float *col_scale;
@@ -171,16 +197,22 @@ static_assert(kGemmSmemBytes <= 232448, "227 KB per CTA");
 struct GemmBars {
     uint64_t full[kGemmMaxStages], empty[kGemmMaxStages];
     uint64_t acc_full[2], acc_empty[2];
-    uint32_t tmem_base;
+    uint32_t tmem_base, last;
 };
 static_assert(sizeof(GemmBars) <= 256, "the barriers' place in shared memory");
 
-struct GemmTile { int job, m0, n0; };
+struct GemmTile { int job, m0, n0, index, part; };
 
 // Tiles of a job in groups of group_m row tiles, all columns of a group before the next group, row tiles fastest: the
 // pairs at work at one time share a few panels of B and the group's rows of A in L2.
+template <bool kSplit>
 __device__ __forceinline__ void gemm_tile_at(const GemmJob &p, int t, GemmTile &at)
 {
+    if constexpr (kSplit) {
+        at.part = t % p.splits;
+        t /= p.splits;
+        at.index = t;
+    }
     const int per = p.group_m * p.tiles_n;
     const int g = t / per, r = t - g * per;
     const int gm = min(p.group_m, p.tiles_m - g * p.group_m);
@@ -189,12 +221,18 @@ __device__ __forceinline__ void gemm_tile_at(const GemmJob &p, int t, GemmTile &
     at.n0 = n * p.width;
 }
 
+// first k-step of a tile's part of K, and the one behind its last
+template <bool kSplit>
+__device__ __forceinline__ int gemm_first(const GemmJob &p, const GemmTile &at) { return kSplit ? at.part * p.ksteps / p.splits : 0; }
+template <bool kSplit>
+__device__ __forceinline__ int gemm_end(const GemmJob &p, const GemmTile &at) { return kSplit ? (at.part + 1) * p.ksteps / p.splits : p.ksteps; }
+
 // The i-th tile of a CTA pair; false behind its last.  Job 0's tiles go round the pairs; the pairs that get one less of
 // them take `extra` tiles of jobs 1 and 2 for it (as many as cost the same), whose remaining ones go round all pairs.
-template <bool kJobs>
+template <bool kJobs, bool kSplit>
 __device__ __forceinline__ bool gemm_tile(const GemmArgs &p, int i, int pair, int pairs, GemmTile &at)
 {
-    const int n0 = p.job[0].tiles_m * p.job[0].tiles_n;
+    const int n0 = p.job[0].tiles_m * p.job[0].tiles_n * (kSplit ? p.job[0].splits : 1);
     int t = pair + i * pairs;
     at.job = 0;
     if constexpr (kJobs) {
@@ -208,12 +246,12 @@ __device__ __forceinline__ bool gemm_tile(const GemmArgs &p, int i, int pair, in
             if (t >= n1 + n2) return false;
             at.job = t < n1 ? 1 : 2;
             if (t >= n1) t -= n1;
-            gemm_tile_at(p.job[at.job], t, at);
+            gemm_tile_at<kSplit>(p.job[at.job], t, at);
             return true;
         }
     }
     if (t >= n0) return false;
-    gemm_tile_at(p.job[0], t, at);
+    gemm_tile_at<kSplit>(p.job[0], t, at);
     return true;
 }
 
@@ -243,7 +281,8 @@ __device__ __forceinline__ void gemm_store_rows(void *to, long long pitch_bytes,
 // 64 threads in two whole warps
 __device__ __forceinline__ void barrier_sync_64(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
-template <int kEpi, bool kI8>
+// kSplit: job 0's K cut into parts.  (A form of its own: the same code under a branch took 0.4 to 0.9 us from every other call.)
+template <int kEpi, bool kI8, bool kSplit>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) weave_gemm_kernel(const __grid_constant__ GemmArgs p)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -282,7 +321,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
         fence_proxy_async_global();      // what the launch before wrote with ordinary stores is read by tensor copies
         int s = 0;
         uint32_t ph = 0;
-        for (int i = 0; ok && gemm_tile<kJobs>(p, i, pair, pairs, at); ++i) {
+        for (int i = 0; ok && gemm_tile<kJobs, kSplit>(p, i, pair, pairs, at); ++i) {
             for (int phase = 0; phase < kPhases && ok; ++phase) {
                 const GemmJob &job = p.job[kPhases == 2 ? phase : at.job];
                 const bool dh = kPhases == 2 && phase == 0;
@@ -294,8 +333,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                 const int mn = load_a ? at.m0 + (int)rank * job.rows : at.n0 + (kGatedTile && !dh ? 0 : (int)rank * half);
                 const bool mn_major = load_a ? a_mn : b_mn;
                 const bool second = load_a ? a_mn : b_boxes == 2;
-                const int ks = job.ksteps;
-                for (int k = 0; k < ks; ++k) {
+                const int from = gemm_first<kSplit>(job, at), to = gemm_end<kSplit>(job, at);
+                for (int k = from; k < to; ++k) {
                     ok = __all_sync(0xffffffffu, ffn_wait(&bars.empty[s], ph ^ 1u, wc, 1 + warp));
                     if (!ok) break;
                     const uint32_t dst = smem + s * p.stage_bytes + (load_a ? 0 : p.a_bytes);
@@ -316,7 +355,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
             // ---- the pair's issuer
             int s = 0;
             uint32_t ph = 0;
-            for (int n = 0; ok && gemm_tile<kJobs>(p, n, pair, pairs, at); ++n) {
+            for (int n = 0; ok && gemm_tile<kJobs, kSplit>(p, n, pair, pairs, at); ++n) {
                 // kEpiGrad: g and u in columns 0-255, dh in 256-383 or 384-511: the next tile's dh is summed up
                 // while the epilogue still reads this one's
                 const int buf = n & 1;
@@ -335,14 +374,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                     const uint32_t idesc = (kI8 ? umma_idesc_i8(256, n_mma) : umma_idesc_bf16(256, n_mma)) | (a_mn ? kIdescAMn : 0u) |
                                            (b_mn ? kIdescBMn : 0u);
                     const uint64_t a_inc = a_mn ? 128 : 2, b_inc = b_mn ? 128 : 2;
-                    const int ks = job.ksteps;
-                    for (int k = 0; k < ks; ++k) {
+                    const int from = gemm_first<kSplit>(job, at), to = gemm_end<kSplit>(job, at);
+                    for (int k = from; k < to; ++k) {
                         ok = __all_sync(0xffffffffu, ffn_wait(&bars.full[s], ph, wc, 4));
                         if (!ok) break;
                         tc_fence_after();
                         const uint32_t a = smem + s * p.stage_bytes, b = a + p.a_bytes;      // (128 rows are read from a on, whatever lies there)
                         ffn_mma_kstep_pair<kI8>(d, a_mn ? umma_desc_mn_sw128(a) : umma_desc_sw128(a),
-                                                b_mn ? umma_desc_mn_sw128(b) : umma_desc_sw128(b), a_inc, b_inc, idesc, (uint32_t)(k != 0),
+                                                b_mn ? umma_desc_mn_sw128(b) : umma_desc_sw128(b), a_inc, b_inc, idesc, (uint32_t)(k != from),
                                                 &bars.empty[s]);
                         if (++s == p.stages) { s = 0; ph ^= 1u; }
                     }
@@ -361,12 +400,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
         float *const scales = reinterpret_cast<float *>(smem_g + kGemmSmemStaging + (warp - 4) * kGemmStaging);      // before results lie there
         const uint32_t empty0 = mapa_u32(smem_u32(&bars.acc_empty[0]), 0);
         pdl_wait();
-        for (int n = 0; gemm_tile<kJobs>(p, n, pair, pairs, at); ++n) {
+        for (int n = 0; gemm_tile<kJobs, kSplit>(p, n, pair, pairs, at); ++n) {
             const GemmJob &job = p.job[at.job];
             const int N = job.N, width = job.width, n0 = at.n0, buf = n & 1;
             const int row0 = at.m0 + (int)rank * job.rows + quarter * 32;
             const int rows = min(min(32, job.rows - quarter * 32), job.M - row0);       // the warp's; may be none
             ok = __all_sync(0xffffffffu, ffn_wait(&bars.acc_full[buf], (n >> 1) & 1, wc, 5));
+            const bool split = kSplit && job.splits > 1;
+            if (split) ok = named_barrier_and<6, 256>(ok);        // barriers follow: all of them or none
             if (!ok) break;
             tc_fence_after();
             // accumulator read: hand it back to the pair's issuer
@@ -375,7 +416,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                 __syncwarp();
                 if (lane == 0) mbar_arrive_remote(kEpi == kEpiGrad ? empty0 : empty0 + buf * 8);
             };
-            if (rows <= 0) {
+            if (rows <= 0 && !split) {
                 release();
                 continue;
             }
@@ -384,14 +425,54 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
 
             if constexpr (kEpi == kEpiStore || kEpi == kEpiScaled) {
                 const int last = min((width - 1) / 64, (N - 1 - n0) / 64);
-                if (group > last) release();
+                const size_t part_words = (size_t)((width + 63) / 64) * 64 * 128 * 2;        // of a pair
+                const uint32_t *const sums = p.partials + (size_t)at.index * job.splits * part_words + rank * (part_words / 2) + quarter * 32 + lane;
+                if (split) {
+                    // this part's sums; whoever is last adds them all up
+                    uint32_t *const mine = const_cast<uint32_t *>(sums) + at.part * part_words;
+                    for (int c = group; c <= last; c += 2) {
+                        uint32_t v[64];
+                        tmem_ld_32x64(lane_base + buf * 256 + c * 64, v);
+                        tmem_ld_wait64(v);
+                        if (rows > 0)
+#pragma unroll
+                            for (int i = 0; i < 64; ++i) __stcg(mine + (size_t)(c * 64 + i) * 128, v[i]);
+                    }
+                    release();
+                    __threadfence();
+                    named_barrier_sync<6, 256>();
+                    if (threadIdx.x == 128) {
+                        unsigned *const arrived = &p.ctl->arrived[at.index * 2 + rank];
+                        bars.last = atom_acqrel_add_u32(arrived, 1u) == (unsigned)job.splits - 1u;
+                        if (bars.last) *arrived = 0u;
+                    }
+                    named_barrier_sync<6, 256>();
+                    if (!bars.last || rows <= 0) continue;
+                    __threadfence();
+                } else if (group > last) {
+                    release();
+                }
 #pragma unroll 1
                 for (int c = group; c <= last; c += 2) {
                     const int col = n0 + c * 64, cols = min(min(64, width - c * 64), N - col);
                     uint32_t v[64];
-                    tmem_ld_32x64(lane_base + buf * 256 + c * 64, v);
-                    tmem_ld_wait64(v);
-                    if (c + 2 > last) release();
+                    if (split) {
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) v[i] = __ldcg(sums + (size_t)(c * 64 + i) * 128);
+#pragma unroll 1
+                        for (int part = 1; part < job.splits; ++part) {
+                            const uint32_t *const from = sums + part * part_words + (size_t)c * 64 * 128;
+#pragma unroll
+                            for (int i = 0; i < 64; ++i) {
+                                const uint32_t w = __ldcg(from + i * 128);
+                                v[i] = kI8 ? v[i] + w : __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w));
+                            }
+                        }
+                    } else {
+                        tmem_ld_32x64(lane_base + buf * 256 + c * 64, v);
+                        tmem_ld_wait64(v);
+                        if (c + 2 > last) release();
+                    }
                     if constexpr (kEpi == kEpiScaled) {
                         __syncwarp();
                         scales[lane] = lane < cols ? p.col_scale[col + lane] : 0.0f;

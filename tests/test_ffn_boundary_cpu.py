@@ -46,6 +46,13 @@ def test_block_shapes(lib):
 
 
 def test_linear_shapes(lib):
+    # partial sums have a place from 33 tokens on, and none where all columns make more than half a wave of tiles
+    def step(f):
+        return f(33) - f(32)
+    assert 9 << 20 < step(lambda T: pk.int8_linear_workspace_bytes(4096, 4096, T)) < 10 << 20
+    assert step(lambda T: pk.int8_linear_workspace_bytes(4096, 14336, T)) < 1 << 17
+    assert 9 << 20 < step(lambda T: pk.ffn_workspace_bytes(4096, 1408, T)) < 10 << 20
+    assert step(lambda T: pk.ffn_workspace_bytes(8192, 1408, T)) < 1 << 17
     assert pk.int8_linear_workspace_bytes(16, 1, 1) > 0
     for bad in ((8, 1, 1), (0, 1, 1), (16, 0, 1), (16, 1, 0), (65552, 1, 1), (16, (1 << 22) + 1, 1), (16, 1, (1 << 22) + 1)):
         assert pk.int8_linear_workspace_bytes(*bad) == 0, bad

@@ -504,6 +504,45 @@ def test_small_batches_of_every_plan(T):
         ffn.close()
 
 
+@pytest.mark.parametrize("T,H,I", [(130, 264, 8120), (257, 72, 6400), (270, 1016, 14840), (596, 136, 4104)])
+def test_long_products_with_few_tiles(T, H, I):
+    """K cut into parts that different thread blocks sum up: forward, gradient, 8-bit; twice, since the arrivals' counters go back to
+    zero, and with another number of rows in between."""
+    x, gate_up, down, dy = block(T, H, I, seed=T + I)
+    ffn = pk.GatedFFN(gate_up, down, max_tokens=T, backward=True)
+    y = ffn.forward(x)
+    within(y, *forward_and_bound(x, gate_up, down))
+    grads = ffn.backward(x, dy)
+    within(ffn.forward(x[: T - 1]), *forward_and_bound(x[: T - 1], gate_up, down))
+    assert torch.equal(ffn.forward(x), y)
+    assert all(torch.equal(a, b) for a, b in zip(ffn.backward(x, dy), grads))
+    ffn.check()
+    # dx once more, in 64 bits from the kernel's own definition
+    g, u, s, h, eg, eu, eh = gated_and_bound(x, gate_up)
+    w, d, dyd = gate_up.double(), down.double(), dy.double()
+    dh = dyd @ d
+    edh = H * STEP * abs_mm(dyd, d)
+    silu, slope = g * s, s * (1 + g * (1 - s))
+    dg, du = dh * u * slope, dh * silu
+    edg = edh * ((u.abs() + eu) * 1.1) + dh.abs() * (eu * 1.1 + (u.abs() + eu) * (0.5 * eg + 3 * ACT * (1 + g.abs()) * s))
+    edu = edh * (silu.abs() + 1.1 * eg) + dh.abs() * (1.1 * eg + ACT * silu.abs())
+    dgu, e = torch.cat([dg, du], 1), torch.cat([edg, edu], 1)
+    e = e + BF16 * (dgu.abs() + e)
+    want = dgu @ w
+    bound = e @ w.abs() + 2 * I * STEP * abs_mm(dgu, w)
+    within(grads[0], want, bound + BF16 * (want.abs() + bound) + TINY)
+    ffn.close()
+    # 8-bit: exact sums, results of 2 and of 4 bytes, widths that end on whole 16 bytes and not
+    for n in (H, H + 1):
+        q, sx, wq, sw = int8_inputs(T, I // 16 * 16, n, T)
+        lin = pk.Int8Linear(wq, sw, max_tokens=T)
+        for out in (torch.float32, torch.bfloat16):
+            for rows in (T, T - 1, T):
+                assert torch.equal(lin.forward(q[:rows], sx[:rows], out_dtype=out), exact_linear(q, sx, wq, sw).to(out)[:rows])
+        lin.check()
+        lin.close()
+
+
 def test_a_row_does_not_depend_on_the_batch():
     """The same token alone, in a small batch and in a large one: 8-bit products are the same bits, bf16 ones within a rounding."""
     H, I = 1024, 1408
