@@ -52,7 +52,7 @@ size_t weave_ffn_workspace_bytes(const weave_ffn_config *cfg);
 int weave_ffn_create(const weave_ffn_config *cfg, weave_ffn_t *out_handle);
 
 /* out[t] = Wd ( silu(Wg x[t]) (.) Wu x[t] ), x and out bf16 [T][H], 0 <= T <= max_tokens.
- * WEAVE_BF16: products are summed up in fp32, the gated product is rounded to bf16 (a relative 2^-9 of each value at
+ * WEAVE_BF16: products are summed up in fp32, the gated product is rounded to bf16 (a relative 2^-8 of each value at
  * most), the result as well.
  * WEAVE_INT8: x is rounded to 8-bit integers with one scale per token (weave_int8_quantize()), so is the gated product
  * behind its rounding to bf16; sums of integer products are exact. */

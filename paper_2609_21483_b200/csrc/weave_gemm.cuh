@@ -128,6 +128,19 @@ __device__ __forceinline__ void ffn_mma_kstep_pair(uint32_t d_tmem, uint64_t a_d
 }
 
 // a barrier of some of the CTA's warps that also says whether all of their threads brought `true`
+__device__ __forceinline__ bool barrier_and_64(int id, bool mine)
+{
+    uint32_t all;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "bar.red.and.pred q, %2, 64, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(all)
+        : "r"((uint32_t)mine), "r"(id)
+        : "memory");
+    return all != 0;
+}
 template <int ID, int THREADS>
 __device__ __forceinline__ bool named_barrier_and(bool mine)
 {
@@ -407,7 +420,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
             const int rows = min(min(32, job.rows - quarter * 32), job.M - row0);       // the warp's; may be none
             ok = __all_sync(0xffffffffu, ffn_wait(&bars.acc_full[buf], (n >> 1) & 1, wc, 5));
             const bool split = kSplit && job.splits > 1;
-            if (split) ok = named_barrier_and<6, 256>(ok);        // barriers follow: all of them or none
+            // where barriers follow, all of those who meet there go on or none
+            if (split) ok = named_barrier_and<6, 256>(ok);
+            if (kEpi == kEpiGrad) ok = barrier_and_64(1 + quarter, ok);
             if (!ok) break;
             tc_fence_after();
             // accumulator read: hand it back to the pair's issuer
