@@ -112,10 +112,12 @@ int engine_create(Engine &e, void *workspace)
     return WEAVE_OK;
 }
 
-// The control words follow the workspace's last use on the stream: none yet, so a synchronous clear.
+// Zeroes the control words, behind all work on the device that was given out before: an allocator may have made the workspace of
+// memory that kernels in flight on some stream still write to.
 int engine_clear(Engine &e, size_t bytes)
 {
-    cudaError_t err = cudaMemset(e.ctl, 0, bytes);
+    cudaError_t err = cudaDeviceSynchronize();
+    if (err == cudaSuccess) err = cudaMemset(e.ctl, 0, bytes);
     if (err == cudaSuccess) err = cudaDeviceSynchronize();
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(e, err);
 }

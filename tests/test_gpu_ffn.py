@@ -393,6 +393,34 @@ def test_on_a_side_stream_and_back_to_back():
     ffn.close()
 
 
+@pytest.mark.parametrize("int8", [False, True])
+def test_made_of_memory_that_is_still_written_to(int8):
+    """The allocator gives a handle the block of a tensor whose last kernel has not run yet."""
+    H, I, T = 256, 512, 16
+    x, gate_up, down, _ = block(T, H, I, seed=13)
+    (gq, gs), (dq, ds) = pk.quantize_rows(gate_up), pk.quantize_rows(down)
+    make = (lambda: pk.Int8FFN(gq, gs, dq, ds, max_tokens=T)) if int8 else (lambda: pk.GatedFFN(gate_up, down, max_tokens=T))
+    ffn = make()
+    want = ffn.forward(x)
+    ffn.check()
+    nbytes = ffn.workspace.numel()
+    ffn.close()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        before = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        torch.cuda._sleep(50_000_000)
+        before.fill_(255)
+        at = before.data_ptr()
+        del before
+        ffn = make()
+        assert ffn.workspace.data_ptr() == at
+        y = ffn.forward(x)
+        ffn.check()
+        assert torch.equal(y, want)
+        ffn.close()
+
+
 def test_refusals_on_the_device():
     x, gate_up, down, dy = block(8, 64, 64)
     ffn = pk.GatedFFN(gate_up, down, max_tokens=8)
