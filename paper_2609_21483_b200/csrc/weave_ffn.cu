@@ -298,10 +298,10 @@ double gemm_tile_us(int ksteps, int accumulator_columns)
 }
 long long gemm_tiles(int M, int N, int width) { return (long long)((M + 255) / 256) * ((N + width - 1) / width); }
 // K is split over pairs where tiles are few and K is long: parts of at least eight steps, all of them in one wave.  (us
-// whole / split: T = 128, 1016 x 14840: 62.5 / 38.4; T = 270: 72.1 / 49.5; 4096 x 14336: T = 128 92.7 / 82.1, T = 200 96.6 /
-// 86.3; gradient T = 596, 264 x 8120: 71.9 / 47.1; 8 bits T = 257, 14336 -> 520: 28.4 / 19.1.)  Whoever adds the parts up
+// whole / split: T = 128, 1016 x 14840: 62.5 / 36.9; T = 270: 72.1 / 50.5; 4096 x 14336: T = 128 92.7 / 82.1, T = 200 96.6 /
+// 86.3; gradient T = 596, 264 x 8120: 71.9 / 47.1; 8 bits T = 257, 14336 -> 520: 28.4 / 17.7.)  Whoever adds the parts up
 // needs a few round trips and reads them all.
-double gemm_join_us(int splits, int width) { return 3.0 + splits * width * 512 / 60000.0; }
+double gemm_join_us(int splits, int width) { return 3.0 + splits * width * 512 / 36000.0; }
 int gemm_splits(const Engine &e, long long tiles, int ksteps, int width)        // at most
 {
     if (width > kGemmSplitWidth || !e.partials) return 1;

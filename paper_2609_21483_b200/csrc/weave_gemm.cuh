@@ -294,6 +294,92 @@ __device__ __forceinline__ void gemm_store_rows(void *to, long long pitch_bytes,
 // 64 threads in two whole warps
 __device__ __forceinline__ void barrier_sync_64(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
+// Rows of up to kCols accumulator columns, scaled where there are scales, as the result's type to where they belong.
+// Lane = row; `stage` is the warp's, `scales` the same place before results lie there.
+template <int kEpi, int kCols>
+__device__ __forceinline__ void gemm_finish(const GemmArgs &p, const GemmJob &job, uint32_t (&v)[kCols], int row0, int rows, int col, int cols, float sx,
+                                            uint32_t stage, float *scales, int lane)
+{
+    if constexpr (kEpi == kEpiScaled) {
+        __syncwarp();
+        scales[lane] = lane < cols ? p.col_scale[col + lane] : 0.0f;
+        if (kCols == 64) scales[lane + 32] = lane + 32 < cols ? p.col_scale[col + 32 + lane] : 0.0f;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kCols; i += 4) {
+            const float4 w = *reinterpret_cast<const float4 *>(scales + i);
+            v[i] = __float_as_uint(__int2float_rn((int)v[i]) * (sx * w.x));
+            v[i + 1] = __float_as_uint(__int2float_rn((int)v[i + 1]) * (sx * w.y));
+            v[i + 2] = __float_as_uint(__int2float_rn((int)v[i + 2]) * (sx * w.z));
+            v[i + 3] = __float_as_uint(__int2float_rn((int)v[i + 3]) * (sx * w.w));
+        }
+    }
+    const bool f32 = kEpi == kEpiScaled && p.out_f32;
+    if (kEpi == kEpiScaled && p.direct) {
+        // rows that start anywhere: a warp's stores of one row lie side by side
+        float *const out_f = static_cast<float *>(job.out);
+        __nv_bfloat16 *const out_b = static_cast<__nv_bfloat16 *>(job.out);
+#pragma unroll
+        for (int half = 0; half < kCols / 32; ++half) {
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) st_shared_u32(stage + lane * 128 + ((i ^ lane) << 2), v[half * 32 + i]);
+            __syncwarp();
+            const int cc = half * 32 + lane;
+            if (cc < cols)
+#pragma unroll 8
+                for (int r = 0; r < rows; ++r) {
+                    const float y = ld_shared_f32(stage + r * 128 + ((lane ^ r) << 2));
+                    const long long to = (long long)(row0 + r) * job.ld + col + cc;
+                    if (f32) out_f[to] = y;
+                    else out_b[to] = __float2bfloat16_rn(y);
+                }
+        }
+    } else if (f32) {
+#pragma unroll
+        for (int half = 0; half < kCols / 32; ++half) {
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                st_shared_v4(gemm_staged(stage, lane, j), make_uint4(v[half * 32 + j * 4], v[half * 32 + j * 4 + 1],
+                                                                       v[half * 32 + j * 4 + 2], v[half * 32 + j * 4 + 3]));
+            __syncwarp();
+            gemm_store_rows<8>(static_cast<float *>(job.out) + row0 * job.ld + col + half * 32, job.ld * 4, rows,
+                               (cols - half * 32) * 4, stage, lane, 0);
+        }
+    } else {
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < kCols / 8; ++j) {
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                w[q] = pack_bf16x2(__uint_as_float(v[j * 8 + q * 2]), __uint_as_float(v[j * 8 + q * 2 + 1]));
+            st_shared_v4(gemm_staged(stage, lane, j), make_uint4(w[0], w[1], w[2], w[3]));
+        }
+        __syncwarp();
+        gemm_store_rows<8>(static_cast<__nv_bfloat16 *>(job.out) + row0 * job.ld + col, job.ld * 2, rows, cols * 2, stage, lane, 0);
+    }
+}
+
+// The parts' sums of up to 32 columns, added up in the order of K; then as above.
+template <int kEpi, bool kI8>
+__device__ __forceinline__ void gemm_join(const GemmArgs &p, const GemmJob &job, const uint32_t *sums, size_t part_words, int row0, int rows, int col,
+                                          int cols, float sx, uint32_t stage, float *scales, int lane)
+{
+    uint32_t v[32], w[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __ldcg(sums + i * 128);
+#pragma unroll 1
+    for (int part = 1; part < job.splits; ++part) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) w[i] = __ldcg(sums + part * part_words + i * 128);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = kI8 ? v[i] + w[i] : __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
+    }
+    gemm_finish<kEpi, 32>(p, job, v, row0, rows, col, cols, sx, stage, scales, lane);
+}
+
 // kSplit: job 0's K cut into parts.  (A form of its own: the same code under a branch took 0.4 to 0.9 us from every other call.)
 template <int kEpi, bool kI8, bool kSplit>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) weave_gemm_kernel(const __grid_constant__ GemmArgs p)
@@ -419,7 +505,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
             const int row0 = at.m0 + (int)rank * job.rows + quarter * 32;
             const int rows = min(min(32, job.rows - quarter * 32), job.M - row0);       // the warp's; may be none
             ok = __all_sync(0xffffffffu, ffn_wait(&bars.acc_full[buf], (n >> 1) & 1, wc, 5));
-            const bool split = kSplit && job.splits > 1;
+            const bool split = kSplit && (kEpi == kEpiScaled || job.splits > 1);
             // where barriers follow, all of those who meet there go on or none
             if (split) ok = named_barrier_and<6, 256>(ok);
             if (kEpi == kEpiGrad) ok = barrier_and_64(1 + quarter, ok);
@@ -439,19 +525,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
             if constexpr (kI8) sx = lane < rows ? p.row_scale[row0 + lane] : 0.0f;
 
             if constexpr (kEpi == kEpiStore || kEpi == kEpiScaled) {
-                const int last = min((width - 1) / 64, (N - 1 - n0) / 64);
-                const size_t part_words = (size_t)((width + 63) / 64) * 64 * 128 * 2;        // of a pair
-                const uint32_t *const sums = p.partials + (size_t)at.index * job.splits * part_words + rank * (part_words / 2) + quarter * 32 + lane;
                 if (split) {
-                    // this part's sums; whoever is last adds them all up
-                    uint32_t *const mine = const_cast<uint32_t *>(sums) + at.part * part_words;
-                    for (int c = group; c <= last; c += 2) {
-                        uint32_t v[64];
-                        tmem_ld_32x64(lane_base + buf * 256 + c * 64, v);
-                        tmem_ld_wait64(v);
+                    // this part's sums; whoever is last adds them all up.  32 columns by each group in turn, so that both have some in
+                    // narrow tiles.  (64 at a time: 25.3 instead of 22.1 us for T = 128, 264 x 8120, 17.5 instead of 15.7 for 100 x
+                    // 14336 -> 520 in 8 bits, the same in wide ones; loads of two parts at a time: within 3 % either way.)
+                    const size_t part_words = (size_t)((width + 63) / 64) * 64 * 128 * 2;        // of a pair
+                    uint32_t *const sums = p.partials + (size_t)at.index * job.splits * part_words + rank * (part_words / 2) + quarter * 32 + lane;
+                    const int there = min(width, N - n0);
+                    for (int c = group * 32; c < there; c += 64) {
+                        uint32_t v[32];
+                        tmem_ld_32x32(lane_base + buf * 256 + c, v);
+                        tmem_ld_wait32(v);
                         if (rows > 0)
 #pragma unroll
-                            for (int i = 0; i < 64; ++i) __stcg(mine + (size_t)(c * 64 + i) * 128, v[i]);
+                            for (int i = 0; i < 32; ++i) __stcg(sums + at.part * part_words + (size_t)(c + i) * 128, v[i]);
                     }
                     release();
                     __threadfence();
@@ -464,90 +551,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                     named_barrier_sync<6, 256>();
                     if (!bars.last || rows <= 0) continue;
                     __threadfence();
-                } else if (group > last) {
-                    release();
+#pragma unroll 1
+                    for (int c = group * 32; c < there; c += 64)
+                        gemm_join<kEpi, kI8>(p, job, sums + (size_t)c * 128, part_words, row0, rows, n0 + c, min(32, there - c), sx, stage, scales, lane);
+                    continue;
                 }
+                const int last = min((width - 1) / 64, (N - 1 - n0) / 64);
+                if (group > last) release();
 #pragma unroll 1
                 for (int c = group; c <= last; c += 2) {
                     const int col = n0 + c * 64, cols = min(min(64, width - c * 64), N - col);
                     uint32_t v[64];
-                    if (split) {
-#pragma unroll
-                        for (int i = 0; i < 64; ++i) v[i] = __ldcg(sums + (size_t)(c * 64 + i) * 128);
-#pragma unroll 1
-                        for (int part = 1; part < job.splits; ++part) {
-                            const uint32_t *const from = sums + part * part_words + (size_t)c * 64 * 128;
-#pragma unroll
-                            for (int i = 0; i < 64; ++i) {
-                                const uint32_t w = __ldcg(from + i * 128);
-                                v[i] = kI8 ? v[i] + w : __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w));
-                            }
-                        }
-                    } else {
-                        tmem_ld_32x64(lane_base + buf * 256 + c * 64, v);
-                        tmem_ld_wait64(v);
-                        if (c + 2 > last) release();
-                    }
-                    if constexpr (kEpi == kEpiScaled) {
-                        __syncwarp();
-                        scales[lane] = lane < cols ? p.col_scale[col + lane] : 0.0f;
-                        scales[lane + 32] = lane + 32 < cols ? p.col_scale[col + 32 + lane] : 0.0f;
-                        __syncwarp();
-#pragma unroll
-                        for (int i = 0; i < 64; i += 4) {
-                            const float4 w = *reinterpret_cast<const float4 *>(scales + i);
-                            v[i] = __float_as_uint(__int2float_rn((int)v[i]) * (sx * w.x));
-                            v[i + 1] = __float_as_uint(__int2float_rn((int)v[i + 1]) * (sx * w.y));
-                            v[i + 2] = __float_as_uint(__int2float_rn((int)v[i + 2]) * (sx * w.z));
-                            v[i + 3] = __float_as_uint(__int2float_rn((int)v[i + 3]) * (sx * w.w));
-                        }
-                    }
-                    const bool f32 = kEpi == kEpiScaled && p.out_f32;
-                    if (kEpi == kEpiScaled && p.direct) {
-                        // rows that start anywhere: a warp's stores of one row lie side by side
-                        float *const out_f = static_cast<float *>(job.out);
-                        __nv_bfloat16 *const out_b = static_cast<__nv_bfloat16 *>(job.out);
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            __syncwarp();
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) st_shared_u32(stage + lane * 128 + ((i ^ lane) << 2), v[half * 32 + i]);
-                            __syncwarp();
-                            const int cc = half * 32 + lane;
-                            if (cc < cols)
-#pragma unroll 8
-                                for (int r = 0; r < rows; ++r) {
-                                    const float y = ld_shared_f32(stage + r * 128 + ((lane ^ r) << 2));
-                                    const long long to = (long long)(row0 + r) * job.ld + col + cc;
-                                    if (f32) out_f[to] = y;
-                                    else out_b[to] = __float2bfloat16_rn(y);
-                                }
-                        }
-                    } else if (f32) {
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            __syncwarp();
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                st_shared_v4(gemm_staged(stage, lane, j), make_uint4(v[half * 32 + j * 4], v[half * 32 + j * 4 + 1],
-                                                                                       v[half * 32 + j * 4 + 2], v[half * 32 + j * 4 + 3]));
-                            __syncwarp();
-                            gemm_store_rows<8>(static_cast<float *>(job.out) + row0 * job.ld + col + half * 32, job.ld * 4, rows,
-                                               (cols - half * 32) * 4, stage, lane, 0);
-                        }
-                    } else {
-                        __syncwarp();
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int q = 0; q < 4; ++q)
-                                w[q] = pack_bf16x2(__uint_as_float(v[j * 8 + q * 2]), __uint_as_float(v[j * 8 + q * 2 + 1]));
-                            st_shared_v4(gemm_staged(stage, lane, j), make_uint4(w[0], w[1], w[2], w[3]));
-                        }
-                        __syncwarp();
-                        gemm_store_rows<8>(static_cast<__nv_bfloat16 *>(job.out) + row0 * job.ld + col, job.ld * 2, rows, cols * 2, stage, lane, 0);
-                    }
+                    tmem_ld_32x64(lane_base + buf * 256 + c * 64, v);
+                    tmem_ld_wait64(v);
+                    if (c + 2 > last) release();
+                    gemm_finish<kEpi, 64>(p, job, v, row0, rows, col, cols, sx, stage, scales, lane);
                 }
             } else if constexpr (kEpi == kEpiGated || kEpi == kEpiScaledGated) {
                 const int last = min((width - 1) / 64, (N - 1 - n0) / 64);
