@@ -45,7 +45,7 @@ typedef struct weave_ffn_config {
 
 /* Bytes of device scratch a handle with this config needs (pure host arithmetic on the five integers; 0 = bad shape): h for
  * max_tokens rows, [dg du] beside it for the gradient, and 9.25 MB for partial sums where a product may cut its K into parts
- * (max_tokens above 32 or the gradient, and H up to 4736). */
+ * (max_tokens above 32 or the gradient, and H up to 4736 or I up to 2368). */
 size_t weave_ffn_workspace_bytes(const weave_ffn_config *cfg);
 
 /* Validates the config, encodes the weights' TMA descriptors, zeroes the control words (synchronous). */

@@ -68,7 +68,7 @@ bool outputs_clear(const Range *out, int n_out, const Range *in, int n_in)
 template <int kEpi, bool kI8>
 cudaError_t size_gemm()
 {
-    if constexpr (kEpi == kEpiStore || kEpi == kEpiScaled) {
+    if constexpr (kEpi != kEpiGrad) {
         const cudaError_t err = cudaFuncSetAttribute(weave_gemm_kernel<kEpi, kI8, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmemBytes);
         if (err != cudaSuccess) return err;
     }
@@ -299,7 +299,8 @@ double gemm_tile_us(int ksteps, int accumulator_columns)
 long long gemm_tiles(int M, int N, int width) { return (long long)((M + 255) / 256) * ((N + width - 1) / width); }
 // K is split over pairs where tiles are few and K is long: parts of at least eight steps, all of them in one wave.  (us
 // whole / split: T = 128, 1016 x 14840: 62.5 / 36.9; T = 270: 72.1 / 50.5; 4096 x 14336: T = 128 92.7 / 82.1, T = 200 96.6 /
-// 86.3; gradient T = 596, 264 x 8120: 71.9 / 47.1; 8 bits T = 257, 14336 -> 520: 28.4 / 17.7.)  Whoever adds the parts up
+// 86.3; gradient T = 596, 264 x 8120: 71.9 / 47.1; 8 bits T = 257, 14336 -> 520: 28.4 / 17.7.  In the
+// product with the activation: T = 128, 7168 x 2048: 36.3 / 31.2; T = 100, 8192 x 256: 29.3 / 20.9.)  Whoever adds the parts up
 // needs a few round trips and reads them all.
 double gemm_join_us(int splits, int width) { return 3.0 + splits * width * 512 / 36000.0; }
 int gemm_splits(const Engine &e, long long tiles, int ksteps, int width)        // at most
@@ -310,9 +311,9 @@ int gemm_splits(const Engine &e, long long tiles, int ksteps, int width)        
 }
 // Workspace for it.  Up to 32 tokens the small batches' kernel leaves nothing to gain (within 1 % there), so that a handle for
 // them, of which a model may have hundreds, stays small.
-size_t gemm_split_room(int N, int ksteps, int max_tokens, bool backward)
+size_t gemm_split_room(long long columns, int ksteps, int max_tokens, bool backward)        // columns of accumulators
 {
-    const bool some = (max_tokens > kSplitMinT || backward) && ksteps >= 16 && 2 * ((N + kGemmSplitWidth - 1) / kGemmSplitWidth) <= kGemmSplitUnits;
+    const bool some = (max_tokens > kSplitMinT || backward) && ksteps >= 16 && 2 * ((columns + kGemmSplitWidth - 1) / kGemmSplitWidth) <= kGemmSplitUnits;
     return some ? kGemmSplitBytes : 0;
 }
 struct GemmWidth { int width, splits; double us; };
@@ -323,8 +324,8 @@ GemmWidth gemm_width(const Engine &e, int M, int N, int ksteps, int widest, int 
         const long long tiles = gemm_tiles(M, N, w), pairs = e.n_sm / 2, waves = (tiles + pairs - 1) / pairs;
         const double end = 0.0055 * w * columns, us = waves * gemm_tile_us(ksteps, w * columns) + end;
         if (us < best.us) best = {w, 1, us};
-        for (int s = may_split ? gemm_splits(e, tiles, ksteps, w) : 1; s > 1; --s) {
-            const double split_us = gemm_tile_us((ksteps + s - 1) / s, w) + end + gemm_join_us(s, w);
+        for (int s = may_split ? gemm_splits(e, tiles, ksteps, w * columns) : 1; s > 1; --s) {
+            const double split_us = gemm_tile_us((ksteps + s - 1) / s, w * columns) + end + gemm_join_us(s, w * columns);
             if (split_us < best.us) best = {w, s, split_us};
         }
     }
@@ -397,7 +398,7 @@ cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int jobs, int b_bytes, Lau
         }
         if (jobs > 1) a.extra = (int)(gemm_tile_us(a.job[0].ksteps / a.job[0].splits, a.job[0].width) / gemm_tile_us(a.job[1].ksteps, a.job[1].width) + 0.5);
     }
-    if constexpr (kEpi == kEpiStore || kEpi == kEpiScaled)
+    if constexpr (kEpi != kEpiGrad)
         if (a.job[0].splits > 1) return launch(weave_gemm_kernel<kEpi, kI8, true>, used * 2, kGemmThreads, kGemmSmemBytes, kind, stream, a);
     return launch(weave_gemm_kernel<kEpi, kI8, false>, used * 2, kGemmThreads, kGemmSmemBytes, kind, stream, a);
 }
@@ -452,6 +453,7 @@ FfnLayout ffn_layout(const weave_ffn_config *c)
     L.partials = at;
     const int step = c->weight_type == WEAVE_INT8 ? 128 : 64;
     L.partial_bytes = gemm_split_room(c->hidden, (c->ffn * (c->backward ? 2 : 1) + step - 1) / step, c->max_tokens, c->backward);
+    if (L.partial_bytes == 0) L.partial_bytes = gemm_split_room(2ll * c->ffn, (c->hidden + step - 1) / step, c->max_tokens, false);
     at += L.partial_bytes;
     L.h = at;
     at += up1024(T * (size_t)line_pitch(c->ffn) * 2);
@@ -535,7 +537,7 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     const void *left = i8 ? static_cast<const void *>(xq) : x, *mid = i8 ? static_cast<const void *>(hq) : hbuf;
     cudaError_t err = cudaSuccess;
     const int step = i8 ? 128 : 64;
-    const GemmWidth up_w = gemm_width(h->e, T, I, (H + step - 1) / step, 128, 8, 2, false);
+    const GemmWidth up_w = gemm_width(h->e, T, I, (H + step - 1) / step, 128, 8, 2, T > kSplitMinT);
     const GemmWidth down_w = gemm_width(h->e, T, H, (I + step - 1) / step, 256, 16, 1, T > kSplitMinT);
     if (T <= kSmallMaxT && small_wins(T, 2, i8, small_us(h->e, I, true, H, step, T) + small_us(h->e, H, false, I, step, T), up_w.us + down_w.us)) {
         SmallArgs a;
@@ -559,7 +561,7 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
         !map_k(h->e, g.job[0].b[1], type, up, I, H, wide) || !map_k(h->e, d.job[0].a, type, mid, T, I, rows_a, pitch) ||
         !map_k(h->e, d.job[0].b[0], type, h->cfg.down, H, I, wide_d / 2))
         return WEAVE_ERR_CUDA;
-    gemm_job(g.job[0], T, I, H, step, wide, false, false, hbuf, pitch);
+    gemm_job(g.job[0], T, I, H, step, wide, false, false, hbuf, pitch, up_w.splits);
     gemm_job(d.job[0], T, H, I, step, wide_d, false, false, out, H, down_w.splits);
     g.row_scale = xs;
     g.col_scale = h->cfg.gate_up_scale;

@@ -181,7 +181,7 @@ struct alignas(64) GemmJob {
                              // 64 where B is MN-major (kEpiGrad, too): with 16 of them in a CTA
                              // the products came out wrong, with 32 right
     int tiles_m, tiles_n, group_m;
-    int splits;              // parts of K that are worked on by different pairs (kEpiStore's job 0, kEpiScaled; else 1): fp32 or
+    int splits;              // parts of K that are worked on by different pairs (kEpiStore's job 0, not in kEpiGrad): fp32 or
                              // int32 sums in `partials`, added up in the order of K by whoever arrives last
 };
 
@@ -362,22 +362,49 @@ __device__ __forceinline__ void gemm_finish(const GemmArgs &p, const GemmJob &jo
     }
 }
 
-// The parts' sums of up to 32 columns, added up in the order of K; then as above.
-template <int kEpi, bool kI8>
-__device__ __forceinline__ void gemm_join(const GemmArgs &p, const GemmJob &job, const uint32_t *sums, size_t part_words, int row0, int rows, int col,
-                                          int cols, float sx, uint32_t stage, float *scales, int lane)
+// The parts' sums of 32 columns, added up in the order of K.
+template <bool kI8>
+__device__ __forceinline__ void gemm_join(uint32_t (&v)[32], const uint32_t *sums, size_t part_words, int splits)
 {
-    uint32_t v[32], w[32];
+    uint32_t w[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __ldcg(sums + i * 128);
 #pragma unroll 1
-    for (int part = 1; part < job.splits; ++part) {
+    for (int part = 1; part < splits; ++part) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) w[i] = __ldcg(sums + part * part_words + i * 128);
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = kI8 ? v[i] + w[i] : __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
     }
-    gemm_finish<kEpi, 32>(p, job, v, row0, rows, col, cols, sx, stage, scales, lane);
+}
+
+// h of 32 columns from col on (N: columns of g), packed to bf16.
+template <bool kI8>
+__device__ __forceinline__ void gemm_gate(const GemmArgs &p, uint32_t (&g)[32], uint32_t (&u)[32], uint32_t *packed, int col, int cols, int N, float sx,
+                                          float *scales, int lane)
+{
+    if constexpr (kI8) {
+        const bool there = lane < cols;
+        __syncwarp();
+        scales[lane] = there ? p.col_scale[col + lane] : 0.0f;
+        scales[lane + 32] = there ? p.col_scale[N + col + lane] : 0.0f;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            const float4 wg = *reinterpret_cast<const float4 *>(scales + i);
+            const float4 wu = *reinterpret_cast<const float4 *>(scales + 32 + i);
+            const float fg[4] = {wg.x, wg.y, wg.z, wg.w}, fu[4] = {wu.x, wu.y, wu.z, wu.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                g[i + q] = __float_as_uint(__int2float_rn((int)g[i + q]) * (sx * fg[q]));
+                u[i + q] = __float_as_uint(__int2float_rn((int)u[i + q]) * (sx * fu[q]));
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        packed[i] = pack_bf16x2(gated(__uint_as_float(g[2 * i]), __uint_as_float(u[2 * i])),
+                                gated(__uint_as_float(g[2 * i + 1]), __uint_as_float(u[2 * i + 1])));
 }
 
 // kSplit: job 0's K cut into parts.  (A form of its own: the same code under a branch took 0.4 to 0.9 us from every other call.)
@@ -505,7 +532,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
             const int row0 = at.m0 + (int)rank * job.rows + quarter * 32;
             const int rows = min(min(32, job.rows - quarter * 32), job.M - row0);       // the warp's; may be none
             ok = __all_sync(0xffffffffu, ffn_wait(&bars.acc_full[buf], (n >> 1) & 1, wc, 5));
-            const bool split = kSplit && (kEpi == kEpiScaled || job.splits > 1);
+            const bool split = kSplit && (!kJobs || job.splits > 1);
             // where barriers follow, all of those who meet there go on or none
             if (split) ok = named_barrier_and<6, 256>(ok);
             if (kEpi == kEpiGrad) ok = barrier_and_64(1 + quarter, ok);
@@ -524,36 +551,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
             float sx = 0.0f;
             if constexpr (kI8) sx = lane < rows ? p.row_scale[row0 + lane] : 0.0f;
 
+            // A part's sums, of `columns` of the accumulator; whoever is last adds them all up.  32 columns by each group in turn, so
+            // that both have some in narrow tiles.  (64 at a time: 25.3 instead of 22.1 us for T = 128, 264 x 8120, 17.5 instead of
+            // 15.7 for 100 x 14336 -> 520 in 8 bits, the same in wide ones; loads of two parts at a time: within 3 % either way.)
+            const size_t part_words = (size_t)(((kGatedTile ? 2 : 1) * width + 63) / 64) * 64 * 128 * 2;        // of a pair
+            uint32_t *const sums = p.partials + (size_t)at.index * job.splits * part_words + rank * (part_words / 2) + quarter * 32 + lane;
+            const int there = min(width, N - n0);
+            const auto arrive = [&](int columns) -> bool {
+                for (int c = group * 32; c < columns; c += 64) {
+                    uint32_t v[32];
+                    tmem_ld_32x32(lane_base + buf * 256 + c, v);
+                    tmem_ld_wait32(v);
+                    if (rows > 0)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) __stcg(sums + at.part * part_words + (size_t)(c + i) * 128, v[i]);
+                }
+                release();
+                __threadfence();
+                named_barrier_sync<6, 256>();
+                if (threadIdx.x == 128) {
+                    unsigned *const arrived = &p.ctl->arrived[at.index * 2 + rank];
+                    bars.last = atom_acqrel_add_u32(arrived, 1u) == (unsigned)job.splits - 1u;
+                    if (bars.last) *arrived = 0u;
+                }
+                named_barrier_sync<6, 256>();
+                __threadfence();
+                return bars.last && rows > 0;
+            };
+
             if constexpr (kEpi == kEpiStore || kEpi == kEpiScaled) {
                 if (split) {
-                    // this part's sums; whoever is last adds them all up.  32 columns by each group in turn, so that both have some in
-                    // narrow tiles.  (64 at a time: 25.3 instead of 22.1 us for T = 128, 264 x 8120, 17.5 instead of 15.7 for 100 x
-                    // 14336 -> 520 in 8 bits, the same in wide ones; loads of two parts at a time: within 3 % either way.)
-                    const size_t part_words = (size_t)((width + 63) / 64) * 64 * 128 * 2;        // of a pair
-                    uint32_t *const sums = p.partials + (size_t)at.index * job.splits * part_words + rank * (part_words / 2) + quarter * 32 + lane;
-                    const int there = min(width, N - n0);
+                    if (!arrive(there)) continue;
+#pragma unroll 1
                     for (int c = group * 32; c < there; c += 64) {
                         uint32_t v[32];
-                        tmem_ld_32x32(lane_base + buf * 256 + c, v);
-                        tmem_ld_wait32(v);
-                        if (rows > 0)
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) __stcg(sums + at.part * part_words + (size_t)(c + i) * 128, v[i]);
+                        gemm_join<kI8>(v, sums + (size_t)c * 128, part_words, job.splits);
+                        gemm_finish<kEpi, 32>(p, job, v, row0, rows, n0 + c, min(32, there - c), sx, stage, scales, lane);
                     }
-                    release();
-                    __threadfence();
-                    named_barrier_sync<6, 256>();
-                    if (threadIdx.x == 128) {
-                        unsigned *const arrived = &p.ctl->arrived[at.index * 2 + rank];
-                        bars.last = atom_acqrel_add_u32(arrived, 1u) == (unsigned)job.splits - 1u;
-                        if (bars.last) *arrived = 0u;
-                    }
-                    named_barrier_sync<6, 256>();
-                    if (!bars.last || rows <= 0) continue;
-                    __threadfence();
-#pragma unroll 1
-                    for (int c = group * 32; c < there; c += 64)
-                        gemm_join<kEpi, kI8>(p, job, sums + (size_t)c * 128, part_words, row0, rows, n0 + c, min(32, there - c), sx, stage, scales, lane);
                     continue;
                 }
                 const int last = min((width - 1) / 64, (N - 1 - n0) / 64);
@@ -568,11 +602,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                     gemm_finish<kEpi, 64>(p, job, v, row0, rows, col, cols, sx, stage, scales, lane);
                 }
             } else if constexpr (kEpi == kEpiGated || kEpi == kEpiScaledGated) {
-                const int last = min((width - 1) / 64, (N - 1 - n0) / 64);
+                __nv_bfloat16 *const out = static_cast<__nv_bfloat16 *>(job.out) + row0 * job.ld + n0;
+                if (split) {
+                    if (!arrive(2 * width)) continue;
+#pragma unroll 1
+                    for (int c = group * 32; c < there; c += 64) {
+                        const int cols = min(32, there - c);
+                        uint32_t g[32], u[32], packed[16];
+                        gemm_join<kI8>(g, sums + (size_t)c * 128, part_words, job.splits);
+                        gemm_join<kI8>(u, sums + (size_t)(width + c) * 128, part_words, job.splits);
+                        gemm_gate<kI8>(p, g, u, packed, n0 + c, cols, N, sx, scales, lane);
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            st_shared_v4(gemm_staged(stage, lane, j), make_uint4(packed[j * 4], packed[j * 4 + 1], packed[j * 4 + 2], packed[j * 4 + 3]));
+                        __syncwarp();
+                        gemm_store_rows<8>(out + c, job.ld * 2, rows, cols * 2, stage, lane, 0);
+                    }
+                    continue;
+                }
+                const int last = (there - 1) / 64;
                 if (group > last) release();
 #pragma unroll 1
                 for (int c = group; c <= last; c += 2) {
-                    const int col = n0 + c * 64, cols = min(min(64, width - c * 64), N - col);
+                    const int cols = min(64, there - c * 64);
                     uint32_t packed[32];
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
@@ -583,35 +636,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                         tmem_ld_wait32(g);
                         reg_fence32(u);
                         if (c + 2 > last && half == 1) release();
-                        if constexpr (kEpi == kEpiScaledGated) {
-                            const bool there = half * 32 + lane < cols;
-                            __syncwarp();
-                            scales[lane] = there ? p.col_scale[n0 + cc + lane] : 0.0f;
-                            scales[lane + 32] = there ? p.col_scale[N + n0 + cc + lane] : 0.0f;
-                            __syncwarp();
-#pragma unroll
-                            for (int i = 0; i < 32; i += 4) {
-                                const float4 wg = *reinterpret_cast<const float4 *>(scales + i);
-                                const float4 wu = *reinterpret_cast<const float4 *>(scales + 32 + i);
-                                const float fg[4] = {wg.x, wg.y, wg.z, wg.w}, fu[4] = {wu.x, wu.y, wu.z, wu.w};
-#pragma unroll
-                                for (int q = 0; q < 4; ++q) {
-                                    g[i + q] = __float_as_uint(__int2float_rn((int)g[i + q]) * (sx * fg[q]));
-                                    u[i + q] = __float_as_uint(__int2float_rn((int)u[i + q]) * (sx * fu[q]));
-                                }
-                            }
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            packed[half * 16 + i] = pack_bf16x2(gated(__uint_as_float(g[2 * i]), __uint_as_float(u[2 * i])),
-                                                                gated(__uint_as_float(g[2 * i + 1]), __uint_as_float(u[2 * i + 1])));
+                        gemm_gate<kI8>(p, g, u, packed + half * 16, n0 + cc, cols - half * 32, N, sx, scales, lane);
                     }
                     __syncwarp();
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         st_shared_v4(gemm_staged(stage, lane, j), make_uint4(packed[j * 4], packed[j * 4 + 1], packed[j * 4 + 2], packed[j * 4 + 3]));
                     __syncwarp();
-                    gemm_store_rows<8>(static_cast<__nv_bfloat16 *>(job.out) + row0 * job.ld + col, job.ld * 2, rows, cols * 2, stage, lane, 0);
+                    gemm_store_rows<8>(out + c * 64, job.ld * 2, rows, cols * 2, stage, lane, 0);
                 }
             } else {
                 // 64 columns at a time, 32 of them by each of a quarter's two warps, which stage a result's rows side by side

@@ -52,7 +52,8 @@ def test_linear_shapes(lib):
     assert 9 << 20 < step(lambda T: pk.int8_linear_workspace_bytes(4096, 4096, T)) < 10 << 20
     assert step(lambda T: pk.int8_linear_workspace_bytes(4096, 14336, T)) < 1 << 17
     assert 9 << 20 < step(lambda T: pk.ffn_workspace_bytes(4096, 1408, T)) < 10 << 20
-    assert step(lambda T: pk.ffn_workspace_bytes(8192, 1408, T)) < 1 << 17
+    assert 9 << 20 < step(lambda T: pk.ffn_workspace_bytes(8192, 1408, T)) < 10 << 20
+    assert step(lambda T: pk.ffn_workspace_bytes(8192, 14336, T)) < 1 << 17
     assert pk.int8_linear_workspace_bytes(16, 1, 1) > 0
     for bad in ((8, 1, 1), (0, 1, 1), (16, 0, 1), (16, 1, 0), (65552, 1, 1), (16, (1 << 22) + 1, 1), (16, 1, (1 << 22) + 1)):
         assert pk.int8_linear_workspace_bytes(*bad) == 0, bad

@@ -571,6 +571,13 @@ def test_long_products_with_few_tiles(T, H, I):
         lin.close()
 
 
+@pytest.mark.parametrize("T,H,I", [(48, 4096, 64), (130, 8112, 144), (257, 6400, 80), (300, 4096, 512), (520, 8192, 208)])
+def test_long_first_products_with_few_tiles(T, H, I):
+    """The same for the product that ends in the activation, in both types."""
+    test_forward(T, H, I)
+    test_int8_ffn(T, H, I)
+
+
 def test_a_row_does_not_depend_on_the_batch():
     """The same token alone, in a small batch and in a large one: 8-bit products are the same bits, bf16 ones within a rounding."""
     H, I = 1024, 1408
