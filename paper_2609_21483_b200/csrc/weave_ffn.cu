@@ -411,10 +411,20 @@ cudaError_t launch_quant_as(const void *x, int rows, int cols, int8_t *q, float 
                   static_cast<const X *>(x), q, scale, cols);
 }
 template <class X>
+cudaError_t launch_quant_short(const void *x, int rows, int cols, int8_t *q, float *scale, LaunchKind kind, cudaStream_t stream)
+{
+    const bool vec = (long long)cols * (int)sizeof(X) % 16 == 0 && aligned(x, 16) && aligned(q, 16);
+    return launch(vec ? weave_quant_short_kernel<X, true> : weave_quant_short_kernel<X, false>, (rows + 3) / 4, 128, 0, kind, stream,
+                  static_cast<const X *>(x), q, scale, rows, cols);
+}
+template <class X>
 cudaError_t launch_quant_rows(const void *x, int rows, int cols, int8_t *q, float *scale, LaunchKind kind, cudaStream_t stream)
 {
-    // threads with four to eight vectors each; few rows get many threads
+    // threads with four to eight vectors each; few rows get many threads.  Many short rows: a warp each, four warps to a block.
+    // (us, 64 threads in a block of their own / a warp: bf16 16384 x 512: 17.6 / 8.0; 9161 x 672: 10.2 / 6.1; 4096 x 2048: 6.3 /
+    // 6.0; 2048 x 512: 2.9 / 2.5; but 2048 x 2048: 4.1 / 4.5, 1024 x 1024: 2.3 / 2.4.)
     const int vectors = cols / (int)(16 / sizeof(X));
+    if ((vectors <= 128 && rows >= 2048) || (vectors <= 256 && rows >= 4096)) return launch_quant_short<X>(x, rows, cols, q, scale, kind, stream);
     if (vectors <= 512 && rows >= 1024) return launch_quant_as<X, 64>(x, rows, cols, q, scale, kind, stream);
     if (vectors <= 1024 && rows >= 512) return launch_quant_as<X, 128>(x, rows, cols, q, scale, kind, stream);
     return launch_quant_as<X, 256>(x, rows, cols, q, scale, kind, stream);

@@ -84,8 +84,8 @@ __device__ __forceinline__ void quant_put(int8_t *dst, int at, const uint4 &v, c
 }
 
 // One row by kThreads threads (tid from 0), which meet at __syncthreads() or, kNamed, at named barrier 1.  kVec: rows
-// start on 16-byte boundaries and are whole 16-byte vectors long.  kKeep: vectors that a thread keeps.  `part`: one word of shared memory per warp.  The row
-// is read past L1, as another SM may just have written it.
+// start on 16-byte boundaries and are whole 16-byte vectors long.  kKeep: vectors that a thread keeps.  `part`: one word of
+// shared memory per warp.  The row is read past L1, as another SM may just have written it.
 template <class X, int kThreads, int kKeep, bool kVec, bool kNamed>
 __device__ __forceinline__ void quant_row_by(const X *x, int8_t *q, float *scale, long long row, int cols, int tid, uint32_t *part)
 {
@@ -153,6 +153,16 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) weave_quant_kernel(
     pdl_launch_dependents();
     pdl_wait();
     quant_row_by<X, kThreads, 8, kVec, false>(x, q, scale, blockIdx.x, cols, threadIdx.x, part);
+}
+
+// one row per warp, for many short rows: what they cost in blocks of their own is the start of a block
+template <class X, bool kVec>
+__global__ void __launch_bounds__(128, 8) weave_quant_short_kernel(const X *x, int8_t *q, float *scale, int rows, int cols)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (row < rows) quant_row_by<X, 32, 8, kVec, false>(x, q, scale, row, cols, threadIdx.x & 31, nullptr);
 }
 
 }  // namespace weave

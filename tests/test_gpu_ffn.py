@@ -203,6 +203,22 @@ def test_quantize_rows(rows, cols, dtype):
     assert torch.equal(s, want_s) and torch.equal(q, want_q)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols", [(2049, 264), (5001, 675), (4099, 2048), (4096, 1), (2050, 7), (16386, 1024)])
+def test_quantize_many_short_rows(rows, cols, dtype):
+    """Rows that share a thread block: every one its own scale, the last ones of a broken block, a row with NaN among them."""
+    x = normal((rows, cols), 1.0, cols, dtype) * (2.0 ** (torch.arange(rows, device="cuda") % 40 - 20))[:, None].to(dtype)
+    q, s = pk.quantize_rows(x)
+    want_q, want_s = exact_quantised(x)
+    assert torch.equal(s, want_s) and torch.equal(q, want_q)
+    x[rows - 2, 0], x[5] = float("nan"), 0.0
+    q2, s2 = pk.quantize_rows(x)
+    assert bool(torch.isnan(s2[rows - 2])) and not bool(q2[rows - 2].any()) and float(s2[5]) == 0.0 and not bool(q2[5].any())
+    keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+    keep[rows - 2] = keep[5] = False
+    assert torch.equal(q2[keep], q[keep]) and torch.equal(s2[keep], s[keep])
+
+
 def test_quantize_rows_at_its_edges():
     """Ties, rows of zeros, infinities and NaN, the largest and the smallest numbers."""
     rows = [[127.0, 0.5, 1.5, 2.5, -0.5, -1.5, -2.5, 126.5],            # scale 1: ties to even
