@@ -70,6 +70,20 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
 int weave_ffn_status(weave_ffn_t h);
 /* Upper bound in milliseconds for any single in-kernel wait (default 4000). */
 int weave_ffn_set_timeout_ms(weave_ffn_t h, int ms);
+/* Test hook: how a call of T tokens is carried out on a device of n_sm SMs (host arithmetic alone, by the routines that the
+ * call itself uses; of the config the integers are read).  Writes up to max_products records, in the order of the products
+ * (backward: dh; g and u; dx; dgate_up; ddown), and returns how many there are. */
+typedef struct weave_ffn_product {
+    int kernel;          /* 0 = on pairs of SMs, 1 = the one launch for up to 128 tokens                          */
+    int mma_n;           /* N of its tensor-core products                                                        */
+    int tail_n;          /* ... of those behind the last whole block of K, 0 where K has no such tail            */
+    int width;           /* columns of the result in a tile                                                      */
+    int parts;           /* parts of K summed up by different pairs                                              */
+    int blocks;          /* blocks of K side by side in a step (kernel 1)                                        */
+    int tiles;           /* kernel 0: of the result; kernel 1: of a thread block                                 */
+    int mn_run, mn_atom; /* where B's N runs along its rows: elements of it in a CTA, and in a swizzle atom; else 0 */
+} weave_ffn_product;
+int weave_ffn_debug_plan(const weave_ffn_config *cfg, int backward, int T, int n_sm, weave_ffn_product *out, int max_products);
 /* Test hook for the give-up path: thread block `cta` of a call of up to 128 tokens never arrives at a grid barrier, so the
  * bounded waits of all expire and the call ends with WEAVE_ERR_TIMEOUT (-1 = off, the default).  Nothing faults or traps. */
 int weave_ffn_debug_withhold_arrival(weave_ffn_t h, int cta);
@@ -110,6 +124,9 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
                               int out_type, int T, void *cuda_stream);
 int weave_int8_linear_status(weave_int8_linear_t h);
 int weave_int8_linear_set_timeout_ms(weave_int8_linear_t h, int ms);
+/* Test hook: as weave_ffn_debug_plan(). */
+int weave_int8_linear_debug_plan(const weave_int8_linear_config *cfg, int x_type, int T, int n_sm, weave_ffn_product *out,
+                                 int max_products);
 int weave_int8_linear_last_cuda_error(weave_int8_linear_t h);
 int weave_int8_linear_destroy(weave_int8_linear_t h);
 

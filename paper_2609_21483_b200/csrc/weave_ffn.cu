@@ -317,6 +317,10 @@ size_t gemm_split_room(long long columns, int ksteps, int max_tokens, bool backw
     return some ? kGemmSplitBytes : 0;
 }
 struct GemmWidth { int width, splits; double us; };
+// N of a product on a pair of CTAs (M = 256) is a multiple of 16 in bf16 and of 32 in 8-bit integers, 256 at most.
+constexpr int gemm_n_unit(bool i8) { return i8 ? 32 : 16; }
+bool gemm_n_legal(bool i8, int n) { return n >= 32 && n <= 256 && n % gemm_n_unit(i8) == 0; }
+// columns: of the accumulator, that a column of the result takes
 GemmWidth gemm_width(const Engine &e, int M, int N, int ksteps, int widest, int unit, int columns, bool may_split)
 {
     GemmWidth best = {widest, 1, 1e30};
@@ -350,6 +354,44 @@ GemmWidth gemm_width_among(const Engine &e, int M, int N, int ksteps, double oth
     return best;
 }
 
+// How a forward call, and a gradient's two launches, are carried out.
+struct ForwardPlan {
+    bool small;
+    GemmWidth up, down;
+};
+ForwardPlan plan_forward(const Engine &e, bool i8, int H, int I, int T)
+{
+    const int step = i8 ? 128 : 64, unit = gemm_n_unit(i8);
+    ForwardPlan p;
+    p.up = gemm_width(e, T, I, (H + step - 1) / step, 128, unit / 2, 2, T > kSplitMinT);
+    p.down = gemm_width(e, T, H, (I + step - 1) / step, 256, unit, 1, T > kSplitMinT);
+    p.small = T <= kSmallMaxT && small_wins(T, 2, i8, small_us(e, I, true, H, step, T) + small_us(e, H, false, I, step, T), p.up.us + p.down.us);
+    return p;
+}
+struct LinearPlan {
+    bool small;
+    GemmWidth w;
+};
+LinearPlan plan_linear(const Engine &e, int K, int N, int T, bool rounds)
+{
+    LinearPlan p;
+    p.w = gemm_width(e, T, N, (K + 127) / 128, 256, gemm_n_unit(true), 1, T > kSplitMinT);
+    p.small = T <= kSmallMaxT && small_wins(T, 1, rounds, small_us(e, N, false, K, 128, T), p.w.us);
+    return p;
+}
+struct BackwardPlan {
+    int wide;            // of h, dg and du
+    GemmWidth dx;
+};
+BackwardPlan plan_backward(const Engine &e, int H, int I, int T)
+{
+    BackwardPlan p;
+    p.wide = gemm_width(e, T, I, (H + 63) / 64 * 3 / 2, 128, 64, 2, false).width;
+    const double others = (gemm_tiles(2 * I, H, 256) + gemm_tiles(H, I, 256)) * gemm_tile_us((T + 63) / 64, 256);
+    p.dx = gemm_width_among(e, T, H, (2 * I + 63) / 64, others);
+    return p;
+}
+
 // Rows of A per CTA where A is K-major: those of the matrix spread evenly over its tiles.
 int gemm_rows(int M)
 {
@@ -378,6 +420,9 @@ void gemm_job(GemmJob &j, int M, int N, long long K, int step, int width, bool a
 template <int kEpi, bool kI8>
 cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int jobs, int b_bytes, LaunchKind kind, cudaStream_t stream)
 {
+    constexpr int columns = kEpi == kEpiGated || kEpi == kEpiGrad || kEpi == kEpiScaledGated ? 2 : 1;
+    for (int i = 0; i < jobs; ++i)
+        if (!gemm_n_legal(kI8, a.job[i].width * columns)) return cudaErrorInvalidValue;
     a.ctl = e.ctl;
     a.timeout_ns = e.timeout_ns;
     a.partials = e.partials;
@@ -434,6 +479,34 @@ cudaError_t launch_quant(const void *x, int type, int rows, int cols, int8_t *q,
     return type == WEAVE_BF16 ? launch_quant_rows<__nv_bfloat16>(x, rows, cols, q, scale, kind, stream)
                               : launch_quant_rows<float>(x, rows, cols, q, scale, kind, stream);
 }
+
+// ---- the plans as weave_ffn_debug_plan() reports them
+
+Engine engine_planned(int n_sm, size_t partial_bytes)
+{
+    Engine e = {};
+    e.n_sm = (n_sm < kMaxSms ? n_sm : kMaxSms) & ~1;
+    e.partials = partial_bytes ? reinterpret_cast<uint32_t *>(1024) : nullptr;      // only asked whether it is there
+    return e;
+}
+struct Products {
+    weave_ffn_product *out;
+    int max, n;
+    void put(const weave_ffn_product &p)
+    {
+        if (out && n < max) out[n] = p;
+        ++n;
+    }
+    void small(const Engine &e, int columns, bool gated, long long K, int block, int T)
+    {
+        const SmallShape s = small_plan(columns, gated, K, block, T, e.n_sm);
+        put({1, s.kbs * s.box_t, s.tail_at >= 0 ? s.box_t : 0, s.ct, 1, s.kbs, s.rounds, 0, 0});
+    }
+    void pairs(int M, int N, int width, int columns, int parts, bool b_mn)
+    {
+        put({0, width * columns, 0, width, parts, 1, (int)gemm_tiles(M, N, width), b_mn ? width * columns / 2 : 0, b_mn ? 64 : 0});
+    }
+};
 
 }  // namespace
 
@@ -547,9 +620,8 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     const void *left = i8 ? static_cast<const void *>(xq) : x, *mid = i8 ? static_cast<const void *>(hq) : hbuf;
     cudaError_t err = cudaSuccess;
     const int step = i8 ? 128 : 64;
-    const GemmWidth up_w = gemm_width(h->e, T, I, (H + step - 1) / step, 128, 8, 2, T > kSplitMinT);
-    const GemmWidth down_w = gemm_width(h->e, T, H, (I + step - 1) / step, 256, 16, 1, T > kSplitMinT);
-    if (T <= kSmallMaxT && small_wins(T, 2, i8, small_us(h->e, I, true, H, step, T) + small_us(h->e, H, false, I, step, T), up_w.us + down_w.us)) {
+    const ForwardPlan plan = plan_forward(h->e, i8, H, I, T);
+    if (plan.small) {
         SmallArgs a;
         a.products = 0;
         if (!small_product(h->e, a, type, h->cfg.gate_up, left, I, true, H, T, xs, h->cfg.gate_up_scale, hbuf, false,
@@ -563,7 +635,7 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     }
     // the wide products: gate and up with the activation, then down
     GemmArgs g, d;
-    const int wide = up_w.width, wide_d = down_w.width;
+    const int wide = plan.up.width, wide_d = plan.down.width;
     const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * wsize;
     const long long pitch = i8 ? I : line_pitch(I);
     const int rows_a = gemm_rows(T);
@@ -571,8 +643,8 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
         !map_k(h->e, g.job[0].b[1], type, up, I, H, wide) || !map_k(h->e, d.job[0].a, type, mid, T, I, rows_a, pitch) ||
         !map_k(h->e, d.job[0].b[0], type, h->cfg.down, H, I, wide_d / 2))
         return WEAVE_ERR_CUDA;
-    gemm_job(g.job[0], T, I, H, step, wide, false, false, hbuf, pitch, up_w.splits);
-    gemm_job(d.job[0], T, H, I, step, wide_d, false, false, out, H, down_w.splits);
+    gemm_job(g.job[0], T, I, H, step, wide, false, false, hbuf, pitch, plan.up.splits);
+    gemm_job(d.job[0], T, H, I, step, wide_d, false, false, out, H, plan.down.splits);
     g.row_scale = xs;
     g.col_scale = h->cfg.gate_up_scale;
     d.job[0].b[1] = d.job[0].b[0];
@@ -612,7 +684,8 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     uint8_t *hbuf = h->ws + h->L.h, *dgu = h->ws + h->L.dgu;
     // h and [dg du] from x and dy
     GemmArgs g;
-    const int wide = gemm_width(h->e, T, I, (H + 63) / 64 * 3 / 2, 128, 64, 2, false).width;
+    const BackwardPlan plan = plan_backward(h->e, H, I, T);
+    const int wide = plan.wide;
     const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * 2;
     const int rows_a = gemm_rows(T);
     const long long h_pitch = line_pitch(I), dgu_pitch = line_pitch(2ll * I);
@@ -634,13 +707,38 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
          map_mn(h->e, d.job[2].a, dy, T, H) && map_mn(h->e, d.job[2].b[0], hbuf, T, I, h_pitch);
     if (!ok) return WEAVE_ERR_CUDA;
     for (int i = 0; i < 3; ++i) d.job[i].b[1] = d.job[i].b[0];
-    const double others = (gemm_tiles(2 * I, H, 256) + gemm_tiles(H, I, 256)) * gemm_tile_us((T + 63) / 64, 256);
-    const GemmWidth dx_w = gemm_width_among(h->e, T, H, (2 * I + 63) / 64, others);
-    gemm_job(d.job[0], T, H, 2ll * I, 64, dx_w.width, false, true, dx, H, dx_w.splits);
+    gemm_job(d.job[0], T, H, 2ll * I, 64, plan.dx.width, false, true, dx, H, plan.dx.splits);
     gemm_job(d.job[1], 2 * I, H, T, 64, 256, true, true, dgate_up, H);
     gemm_job(d.job[2], H, I, T, 64, 256, true, true, ddown, I);
     err = launch_gemm<kEpiStore, false>(h->e, d, 3, kGemmHalf, kBehind, stream);
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
+}
+
+int weave_ffn_debug_plan(const weave_ffn_config *cfg, int backward, int T, int n_sm, weave_ffn_product *out, int max_products)
+{
+    if (!ffn_shape_ok(cfg) || T < 1 || T > cfg->max_tokens || n_sm < 2 || max_products < 0 || (backward && !cfg->backward)) return WEAVE_ERR_INVALID_ARG;
+    const int H = cfg->hidden, I = cfg->ffn;
+    const bool i8 = cfg->weight_type == WEAVE_INT8;
+    const Engine e = engine_planned(n_sm, ffn_layout(cfg).partial_bytes);
+    Products p = {out, max_products, 0};
+    if (backward) {
+        const BackwardPlan plan = plan_backward(e, H, I, T);
+        p.pairs(T, I, plan.wide, 1, 1, true);        // dh
+        p.pairs(T, I, plan.wide, 2, 1, false);       // g and u
+        p.pairs(T, H, plan.dx.width, 1, plan.dx.splits, true);
+        p.pairs(2 * I, H, 256, 1, 1, true);
+        p.pairs(H, I, 256, 1, 1, true);
+        return p.n;
+    }
+    const ForwardPlan plan = plan_forward(e, i8, H, I, T);
+    if (plan.small) {
+        p.small(e, I, true, H, i8 ? 128 : 64, T);
+        p.small(e, H, false, I, i8 ? 128 : 64, T);
+    } else {
+        p.pairs(T, I, plan.up.width, 2, plan.up.splits, false);
+        p.pairs(T, H, plan.down.width, 1, plan.down.splits, false);
+    }
+    return p.n;
 }
 
 int weave_ffn_status(weave_ffn_t h) { return h ? engine_status(h->e, h->L.control) : WEAVE_ERR_INVALID_ARG; }
@@ -770,8 +868,8 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     const void *q = round ? xq : x;
     if (round) x_scale = xs;
     const bool direct = (size_t)N * out_size % 16 != 0;
-    const GemmWidth w = gemm_width(h->e, T, N, (K + 127) / 128, 256, 16, 1, T > kSplitMinT);
-    if (T <= kSmallMaxT && small_wins(T, 1, round, small_us(h->e, N, false, K, 128, T), w.us)) {
+    const LinearPlan plan = plan_linear(h->e, K, N, T, round);
+    if (plan.small) {
         SmallArgs a;
         a.products = 0;
         if (!small_product(h->e, a, WEAVE_INT8, h->cfg.weight, q, N, false, K, T, x_scale, h->cfg.scale, out, out_type == WEAVE_F32,
@@ -786,7 +884,7 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
         if (err != cudaSuccess) return cuda_fail(h->e, err);
     }
     GemmArgs g;
-    const int wide = w.width;
+    const int wide = plan.w.width;
     const int rows_a = gemm_rows(T);
     g.direct = direct;
     g.out_f32 = out_type == WEAVE_F32;
@@ -794,9 +892,23 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
     g.col_scale = h->cfg.scale;
     if (!map_k(h->e, g.job[0].a, WEAVE_INT8, q, T, K, rows_a) || !map_k(h->e, g.job[0].b[0], WEAVE_INT8, h->cfg.weight, N, K, wide / 2)) return WEAVE_ERR_CUDA;
     g.job[0].b[1] = g.job[0].b[0];
-    gemm_job(g.job[0], T, N, K, 128, wide, false, false, out, N, w.splits);
+    gemm_job(g.job[0], T, N, K, 128, wide, false, false, out, N, plan.w.splits);
     err = launch_gemm<kEpiScaled, true>(h->e, g, 1, wide * 64, round ? kBehind : kPlain, stream);
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(h->e, err);
+}
+
+int weave_int8_linear_debug_plan(const weave_int8_linear_config *cfg, int x_type, int T, int n_sm, weave_ffn_product *out, int max_products)
+{
+    if (!int8_shape_ok(cfg) || (x_type != WEAVE_BF16 && x_type != WEAVE_F32 && x_type != WEAVE_INT8) || T < 1 || T > cfg->max_tokens ||
+        n_sm < 2 || max_products < 0)
+        return WEAVE_ERR_INVALID_ARG;
+    const int K = cfg->in_features, N = cfg->out_features;
+    const Engine e = engine_planned(n_sm, int8_layout(cfg).partial_bytes);
+    Products p = {out, max_products, 0};
+    const LinearPlan plan = plan_linear(e, K, N, T, x_type != WEAVE_INT8);
+    if (plan.small) p.small(e, N, false, K, 128, T);
+    else p.pairs(T, N, plan.w.width, 1, plan.w.splits, false);
+    return p.n;
 }
 
 int weave_int8_linear_status(weave_int8_linear_t h) { return h ? engine_status(h->e, h->L.control) : WEAVE_ERR_INVALID_ARG; }

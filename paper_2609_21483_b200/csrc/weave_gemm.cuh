@@ -177,9 +177,9 @@ struct alignas(64) GemmJob {
     int ksteps;
     int a_mn, b_mn;          // kEpiStore: operand is MN-major
     int rows;                // rows of A that a CTA takes of a tile, a multiple of 8 up to 128: a tile is 2 x rows high
-    int width;               // columns of the result in a tile: a multiple of 16 up to 256, gated of 8 up to 128; of
-                             // 64 where B is MN-major (kEpiGrad, too): with 16 of them in a CTA
-                             // the products came out wrong, with 32 right
+    int width;               // columns of the result in a tile, up to 256 (gated 128): a product's N, twice that in the gated
+                             // forms, is a multiple of 16 in bf16 and of 32 in 8-bit integers.  Of 64 where B is MN-major
+                             // (kEpiGrad, too): with 16 of them in a CTA the products came out wrong, with 32 right
     int tiles_m, tiles_n, group_m;
     int splits;              // parts of K that are worked on by different pairs (kEpiStore's job 0, not in kEpiGrad): fp32 or
                              // int32 sums in `partials`, added up in the order of K by whoever arrives last

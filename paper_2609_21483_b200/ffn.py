@@ -14,10 +14,10 @@ BF16, F32, INT8 = 0, 1, 2
 
 EXPORTS = [
     "weave_ffn_workspace_bytes", "weave_ffn_create", "weave_ffn_forward", "weave_ffn_backward", "weave_ffn_status",
-    "weave_ffn_set_timeout_ms", "weave_ffn_debug_withhold_arrival", "weave_ffn_last_cuda_error", "weave_ffn_destroy",
+    "weave_ffn_set_timeout_ms", "weave_ffn_debug_plan", "weave_ffn_debug_withhold_arrival", "weave_ffn_last_cuda_error", "weave_ffn_destroy",
     "weave_int8_quantize", "weave_int8_linear_workspace_bytes", "weave_int8_linear_create",
     "weave_int8_linear_forward", "weave_int8_linear_status", "weave_int8_linear_set_timeout_ms",
-    "weave_int8_linear_last_cuda_error", "weave_int8_linear_destroy",
+    "weave_int8_linear_debug_plan", "weave_int8_linear_last_cuda_error", "weave_int8_linear_destroy",
 ]
 
 
@@ -33,6 +33,10 @@ class _Int8LinearConfig(ctypes.Structure):
     _fields_ = [("in_features", ctypes.c_int), ("out_features", ctypes.c_int), ("max_tokens", ctypes.c_int),
                 ("weight", ctypes.c_void_p), ("scale", ctypes.c_void_p),
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class _Product(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("kernel", "mma_n", "tail_n", "width", "parts", "blocks", "tiles", "mn_run", "mn_atom")]
 
 
 _lib = None
@@ -53,12 +57,15 @@ def load():
                        ("weave_ffn_forward", [vp, vp, vp, ci, vp]),
                        ("weave_ffn_backward", [vp, vp, vp, vp, vp, vp, ci, vp]),
                        ("weave_ffn_status", [vp]), ("weave_ffn_set_timeout_ms", [vp, ci]),
+                       ("weave_ffn_debug_plan", [ctypes.POINTER(_FfnConfig), ci, ci, ci, ctypes.POINTER(_Product), ci]),
                        ("weave_ffn_debug_withhold_arrival", [vp, ci]),
                        ("weave_ffn_last_cuda_error", [vp]), ("weave_ffn_destroy", [vp]),
                        ("weave_int8_quantize", [vp, ci, ci, ci, vp, vp, vp]),
                        ("weave_int8_linear_create", [ctypes.POINTER(_Int8LinearConfig), vpp]),
                        ("weave_int8_linear_forward", [vp, vp, ci, vp, vp, ci, ci, vp]),
                        ("weave_int8_linear_status", [vp]), ("weave_int8_linear_set_timeout_ms", [vp, ci]),
+                       ("weave_int8_linear_debug_plan",
+                        [ctypes.POINTER(_Int8LinearConfig), ci, ci, ci, ctypes.POINTER(_Product), ci]),
                        ("weave_int8_linear_last_cuda_error", [vp]), ("weave_int8_linear_destroy", [vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = ci, args
@@ -75,6 +82,27 @@ def ffn_workspace_bytes(hidden: int, ffn: int, max_tokens: int, int8: bool = Fal
 def int8_linear_workspace_bytes(in_features: int, out_features: int, max_tokens: int) -> int:
     cfg = _Int8LinearConfig(in_features, out_features, max_tokens)
     return int(load().weave_int8_linear_workspace_bytes(ctypes.byref(cfg)))
+
+
+def _products(fn, *args):
+    out = (_Product * 5)()
+    n = fn(*args, out, 5)
+    if n < 0:
+        raise WeaveError(n, fn.__name__)
+    return [{name: getattr(p, name) for name, _ in _Product._fields_} for p in out[:n]]
+
+
+def ffn_plan(hidden: int, ffn: int, T: int, max_tokens: Optional[int] = None, int8: bool = False, backward: bool = False,
+             n_sm: int = 148):
+    """How a call is carried out, one dict per product (see weave_ffn_debug_plan); needs no GPU."""
+    cfg = _FfnConfig(hidden, ffn, max_tokens or T, INT8 if int8 else BF16, int(backward))
+    return _products(load().weave_ffn_debug_plan, ctypes.byref(cfg), int(backward), T, n_sm)
+
+
+def int8_linear_plan(in_features: int, out_features: int, T: int, max_tokens: Optional[int] = None, x_type: int = BF16,
+                     n_sm: int = 148):
+    cfg = _Int8LinearConfig(in_features, out_features, max_tokens or T)
+    return _products(load().weave_int8_linear_debug_plan, ctypes.byref(cfg), x_type, T, n_sm)
 
 
 _types = {}
