@@ -65,8 +65,9 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
 int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, void *dgate_up, void *ddown, int T,
                        void *cuda_stream);
 
-/* Synchronises the last stream, returns the device status word (WEAVE_OK, or WEAVE_ERR_TIMEOUT if a bounded in-kernel
- * wait gave up, after which results are undefined) and clears it. */
+/* Waits for all work on the device (graphs of the handle's calls may have been replayed on any stream), returns the device
+ * status word (WEAVE_OK, or WEAVE_ERR_TIMEOUT if a bounded in-kernel wait gave up, after which results are undefined) and
+ * clears it. */
 int weave_ffn_status(weave_ffn_t h);
 /* Upper bound in milliseconds for any single in-kernel wait (default 4000). */
 int weave_ffn_set_timeout_ms(weave_ffn_t h, int ms);

@@ -32,7 +32,6 @@ struct Engine {
     FfnCtl *ctl;
     uint32_t *partials;        // kGemmSplitBytes; null where no call splits K
     unsigned long long timeout_ns;
-    cudaStream_t last_stream;
     int last_cuda_error;
     int withhold;              // weave_ffn_debug_withhold_arrival()
     EncodeTiledFn encode;
@@ -96,7 +95,6 @@ int engine_create(Engine &e, void *workspace)
     e.n_sm = (sms < kMaxSms ? sms : kMaxSms) & ~1;
     e.ctl = static_cast<FfnCtl *>(workspace);
     e.timeout_ns = 4000ull * 1000000ull;
-    e.last_stream = nullptr;
     e.last_cuda_error = 0;
     e.withhold = -1;
     void *fn = nullptr;
@@ -122,9 +120,17 @@ int engine_clear(Engine &e, size_t bytes)
     return err == cudaSuccess ? WEAVE_OK : cuda_fail(e, err);
 }
 
+bool on_its_device(const Engine &e)
+{
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == e.device;
+}
+
+// Behind all work on the device: a graph of the handle's calls may have been replayed on any stream.
 int engine_status(Engine &e, size_t control_bytes)
 {
-    cudaError_t err = cudaStreamSynchronize(e.last_stream);
+    if (!on_its_device(e)) return WEAVE_ERR_INVALID_ARG;
+    cudaError_t err = cudaDeviceSynchronize();
     if (err != cudaSuccess) return cuda_fail(e, err);
     int st = 0;
     err = cudaMemcpy(&st, &e.ctl->status, sizeof(st), cudaMemcpyDeviceToHost);
@@ -134,12 +140,6 @@ int engine_status(Engine &e, size_t control_bytes)
         if (rc) return rc;
     }
     return st;
-}
-
-bool on_its_device(const Engine &e)
-{
-    int dev = -1;
-    return cudaGetDevice(&dev) == cudaSuccess && dev == e.device;
 }
 
 // [rows][cols] row-major, rows `pitch` elements apart (0: cols), box of box_cols x box_rows
@@ -611,7 +611,6 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     const Range ins[4] = {{x, rows}, {h->cfg.gate_up, (size_t)2 * I * H * wsize}, {h->cfg.down, (size_t)I * H * wsize}, {h->ws, h->L.total}};
     if (!outputs_clear(outs, 1, ins, 4) || !on_its_device(h->e)) return WEAVE_ERR_INVALID_ARG;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    h->e.last_stream = stream;
     uint8_t *hbuf = h->ws + h->L.h;
     int8_t *xq = reinterpret_cast<int8_t *>(h->ws + h->L.xq), *hq = reinterpret_cast<int8_t *>(h->ws + h->L.hq);
     float *xs = reinterpret_cast<float *>(h->ws + h->L.x_scale), *hs = reinterpret_cast<float *>(h->ws + h->L.h_scale);
@@ -674,7 +673,6 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     const Range ins[5] = {{x, rows}, {dy, rows}, {h->cfg.gate_up, w_gu}, {h->cfg.down, w_d}, {h->ws, h->L.total}};
     if (!outputs_clear(outs, 3, ins, 5) || !on_its_device(h->e)) return WEAVE_ERR_INVALID_ARG;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    h->e.last_stream = stream;
     cudaError_t err;
     if (T == 0) {
         err = cudaMemsetAsync(dgate_up, 0, w_gu, stream);
@@ -860,7 +858,6 @@ int weave_int8_linear_forward(weave_int8_linear_t h, const void *x, int x_type, 
                           {h->cfg.scale, (size_t)N * 4}, {h->ws, h->L.total}};
     if (!outputs_clear(outs, 1, ins, 5) || !on_its_device(h->e)) return WEAVE_ERR_INVALID_ARG;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    h->e.last_stream = stream;
     cudaError_t err;
     int8_t *xq = reinterpret_cast<int8_t *>(h->ws + h->L.xq);
     float *xs = reinterpret_cast<float *>(h->ws + h->L.x_scale);

@@ -166,7 +166,7 @@ class _Handle:
             raise WeaveError(rc, fn.__name__)
 
     def status(self) -> int:
-        """Synchronises the last call's stream; 0, or ERR_TIMEOUT after a wait that gave up, and clears it."""
+        """Waits for all work on the device; 0, or ERR_TIMEOUT after a wait that gave up, and clears it."""
         with self._torch.cuda.device(self.device):
             return int(getattr(self._lib, f"{self._name}_status")(self._h))
 

@@ -1,0 +1,38 @@
+"""The dense block's calls in orders that a program may make them in, and what they refuse."""
+import pytest
+import torch
+
+import paper_2609_21483_b200 as pk
+from test_gpu_ffn import block
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_status_of_a_graph_replayed_on_another_stream(int8):
+    """A captured call whose wait gives up, replayed on a stream that the handle never saw, behind work that is still running."""
+    T, H, I = 5, 1024, 2048
+    x, gate_up, down, _ = block(T, H, I, seed=61)
+    if int8:
+        ffn = pk.Int8FFN(*pk.quantize_rows(gate_up), *pk.quantize_rows(down), max_tokens=T)
+    else:
+        ffn = pk.GatedFFN(gate_up, down, max_tokens=T)
+    want = ffn.forward(x)
+    ffn.check()
+    out = torch.empty_like(x)
+    ffn.set_timeout_ms(20)
+    ffn.debug_withhold_arrival(3)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ffn.forward(x, out=out)
+    ffn.debug_withhold_arrival(-1)
+    ffn.set_timeout_ms(4000)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+        graph.replay()
+    assert ffn.status() == pk.ERR_TIMEOUT
+    assert torch.equal(ffn.forward(x), want)
+    ffn.check()
+    ffn.close()
