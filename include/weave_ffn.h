@@ -12,7 +12,7 @@
  *     by the caller.  That holds for replays of graphs that were captured from the same handle, too.
  *   - The weights may be changed between calls (by work that the stream orders before the next call); the handle keeps
  *     nothing computed from them.
- *   - An output must not overlap an input, a weight, another output or the workspace (WEAVE_ERR_INVALID_ARG).
+ *   - An output must not overlap an input, a weight or its scales, another output or the workspace (WEAVE_ERR_INVALID_ARG).
  *   - T = 0 is allowed: no rows are read or written (a backward call then fills the weight gradients with zeros).
  */
 #ifndef WEAVE_FFN_H

@@ -608,13 +608,14 @@ int weave_ffn_forward(weave_ffn_t h, const void *x, void *out, int T, void *cuda
     if (!x || !out || !aligned(x, 16) || !aligned(out, 16)) return WEAVE_ERR_INVALID_ARG;
     const size_t wsize = h->cfg.weight_type == WEAVE_INT8 ? 1 : 2, rows = (size_t)T * H * 2;
     const Range outs[1] = {{out, rows}};
-    const Range ins[4] = {{x, rows}, {h->cfg.gate_up, (size_t)2 * I * H * wsize}, {h->cfg.down, (size_t)I * H * wsize}, {h->ws, h->L.total}};
-    if (!outputs_clear(outs, 1, ins, 4) || !on_its_device(h->e)) return WEAVE_ERR_INVALID_ARG;
+    const bool i8 = h->cfg.weight_type == WEAVE_INT8;
+    const Range ins[6] = {{x, rows}, {h->cfg.gate_up, (size_t)2 * I * H * wsize}, {h->cfg.down, (size_t)I * H * wsize}, {h->ws, h->L.total},
+                          {h->cfg.gate_up_scale, i8 ? (size_t)2 * I * 4 : 0}, {h->cfg.down_scale, i8 ? (size_t)H * 4 : 0}};
+    if (!outputs_clear(outs, 1, ins, 6) || !on_its_device(h->e)) return WEAVE_ERR_INVALID_ARG;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     uint8_t *hbuf = h->ws + h->L.h;
     int8_t *xq = reinterpret_cast<int8_t *>(h->ws + h->L.xq), *hq = reinterpret_cast<int8_t *>(h->ws + h->L.hq);
     float *xs = reinterpret_cast<float *>(h->ws + h->L.x_scale), *hs = reinterpret_cast<float *>(h->ws + h->L.h_scale);
-    const bool i8 = h->cfg.weight_type == WEAVE_INT8;
     const int type = i8 ? WEAVE_INT8 : WEAVE_BF16;
     const void *left = i8 ? static_cast<const void *>(xq) : x, *mid = i8 ? static_cast<const void *>(hq) : hbuf;
     cudaError_t err = cudaSuccess;

@@ -36,3 +36,18 @@ def test_status_of_a_graph_replayed_on_another_stream(int8):
     assert torch.equal(ffn.forward(x), want)
     ffn.check()
     ffn.close()
+
+
+def test_an_output_on_top_of_scales_is_refused():
+    H, I = 64, 96
+    x, gate_up, down, _ = block(1, H, I, seed=62)
+    gq, gs, dq, ds = *pk.quantize_rows(gate_up), *pk.quantize_rows(down)
+    ffn = pk.Int8FFN(gq, gs, dq, ds, max_tokens=1)
+    for scale in (gs, ds):
+        before = scale.clone()
+        with pytest.raises(pk.WeaveError):
+            ffn.forward(x, out=scale.view(torch.bfloat16)[-H:].view(1, H))
+        torch.cuda.synchronize()
+        assert torch.equal(scale, before)
+    ffn.check()
+    ffn.close()
