@@ -459,7 +459,7 @@ template <class X>
 cudaError_t launch_quant_short(const void *x, int rows, int cols, int8_t *q, float *scale, LaunchKind kind, cudaStream_t stream)
 {
     const bool vec = (long long)cols * (int)sizeof(X) % 16 == 0 && aligned(x, 16) && aligned(q, 16);
-    return launch(vec ? weave_quant_short_kernel<X, true> : weave_quant_short_kernel<X, false>, (rows + 3) / 4, 128, 0, kind, stream,
+    return launch(vec ? weave_quant_short_kernel<X, true> : weave_quant_short_kernel<X, false>, (rows - 1) / 4 + 1, 128, 0, kind, stream,
                   static_cast<const X *>(x), q, scale, rows, cols);
 }
 template <class X>

@@ -51,3 +51,17 @@ def test_an_output_on_top_of_scales_is_refused():
         assert torch.equal(scale, before)
     ffn.check()
     ffn.close()
+
+
+def test_the_largest_number_of_rows():
+    """2^31 - 1 rows of one value each."""
+    rows, part = (1 << 31) - 1, 1 << 28
+    x = torch.empty(rows, 1, dtype=torch.bfloat16, device="cuda")
+    value = lambda at: ((torch.arange(at, min(at + part, rows), device="cuda", dtype=torch.int32) & 255) - 127).to(torch.bfloat16)
+    for at in range(0, rows, part):
+        x[at:at + part, 0] = value(at)
+    q, s = pk.quantize_rows(x)
+    for at in range(0, rows, part):
+        v = value(at)
+        assert torch.equal(q[at:at + part, 0], (torch.sign(v) * 127).to(torch.int8))
+        assert torch.equal(s[at:at + part], (v.double().abs() / 127.0).float())
