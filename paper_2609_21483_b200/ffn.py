@@ -2,6 +2,9 @@
 
 Argument marshalling only, as for the MoE layer: every product and rounding runs inside the CUDA library; PyTorch is
 used for device memory and streams.  There is no CPU or eager fallback.
+
+`stream`: the number (cuda_stream) of the stream that a call runs on; by default the device's current one.  Inputs have to be
+ready there, and results that the call allocates belong to that stream, as if it had been made the current one.
 """
 from __future__ import annotations
 
@@ -115,6 +118,16 @@ def _type_of(dtype):
     return _types[dtype]
 
 
+def _empty(shape, dtype, device, stream: Optional[int]):
+    """A result for a call on `stream` (None: the current one), from that stream's memory: what lies in the current stream's may still
+    be written to by kernels that were launched there before."""
+    import torch
+    if stream is None or stream == torch.cuda.current_stream(device).cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def quantize_rows(x, q=None, scale=None, stream: Optional[int] = None):
     """x [rows, cols] in bf16 or fp32 -> (int8 [rows, cols], fp32 scale [rows]): scale = max|row| / 127, the nearest
     integer to x / scale.  Tokens' activations and weights' output channels alike (see weave_int8_quantize)."""
@@ -122,9 +135,9 @@ def quantize_rows(x, q=None, scale=None, stream: Optional[int] = None):
     assert x.is_cuda and x.dim() == 2 and x.is_contiguous() and x.dtype in (torch.bfloat16, torch.float32)
     rows, cols = x.shape
     if q is None:
-        q = torch.empty(rows, cols, dtype=torch.int8, device=x.device)
+        q = _empty((rows, cols), torch.int8, x.device, stream)
     if scale is None:
-        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+        scale = _empty((rows,), torch.float32, x.device, stream)
     assert q.device == x.device and q.dtype == torch.int8 and q.is_contiguous() and tuple(q.shape) == (rows, cols)
     assert scale.device == x.device and scale.dtype == torch.float32 and scale.is_contiguous() and tuple(scale.shape) == (rows,)
     if stream is None:
@@ -225,7 +238,7 @@ class GatedFFN(_Handle):
     def forward(self, x, out=None, stream: Optional[int] = None):
         """x bf16 [T, H] -> bf16 [T, H]."""
         if out is None:
-            out = self._torch.empty_like(x)
+            out = _empty(x.shape, self._torch.bfloat16, self.device, stream)
         T = self._rows(x, out)
         self._call(self._lib.weave_ffn_forward, x.data_ptr(), out.data_ptr(), T, stream=stream)
         return out
@@ -236,9 +249,8 @@ class GatedFFN(_Handle):
     def backward(self, x, dy, dx=None, dgate_up=None, ddown=None, stream: Optional[int] = None):
         """(dx [T, H], dgate_up [2I, H], ddown [H, I]) in bf16 for the gradient dy of forward(x); all overwritten."""
         torch = self._torch
-        dx = torch.empty_like(x) if dx is None else dx
-        dgate_up = torch.empty_like(self.gate_up) if dgate_up is None else dgate_up
-        ddown = torch.empty_like(self.down) if ddown is None else ddown
+        dx, dgate_up, ddown = (_empty(like.shape, torch.bfloat16, self.device, stream) if g is None else g
+                               for g, like in ((dx, x), (dgate_up, self.gate_up), (ddown, self.down)))
         T = self._rows(x, dy, dx)
         for g, w in ((dgate_up, self.gate_up), (ddown, self.down)):
             assert g.device == self.device and g.dtype == torch.bfloat16 and g.is_contiguous() and g.shape == w.shape
@@ -293,7 +305,7 @@ class Int8Linear(_Handle):
         torch = self._torch
         T = x.shape[0]
         if out is None:
-            out = torch.empty(T, self.N, dtype=out_dtype or torch.bfloat16, device=self.device)
+            out = _empty((T, self.N), out_dtype or torch.bfloat16, self.device, stream)
         assert x.device == self.device and x.is_contiguous() and tuple(x.shape) == (T, self.K)
         assert x.dtype in (torch.bfloat16, torch.float32, torch.int8) and (x.dtype == torch.int8) == (x_scale is not None)
         if x_scale is not None:

@@ -65,3 +65,41 @@ def test_the_largest_number_of_rows():
         v = value(at)
         assert torch.equal(q[at:at + part, 0], (torch.sign(v) * 127).to(torch.int8))
         assert torch.equal(s[at:at + part], (v.double().abs() / 127.0).float())
+
+
+def behind_pending_work(nbytes):
+    """Leaves the allocator a block of the current stream that a kernel, which has yet to run there, still writes to."""
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    block = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    torch.cuda._sleep(50_000_000)
+    block.fill_(255)
+
+
+@pytest.mark.parametrize("call", ["forward", "backward", "int8_ffn", "linear", "quantize"])
+def test_results_of_a_call_on_a_given_stream(call):
+    """What a call allocates for its results is ordered by the stream that the call runs on, not by the current one."""
+    T, H, I = 1000, 1040, 1056
+    x, gate_up, down, dy = block(T, H, I, seed=63)
+    gq, gs, dq, ds = *pk.quantize_rows(gate_up), *pk.quantize_rows(down)
+    ffn = pk.GatedFFN(gate_up, down, max_tokens=T, backward=True)
+    i8, lin = pk.Int8FFN(gq, gs, dq, ds, max_tokens=T), pk.Int8Linear(gq, gs, max_tokens=T)
+    run = {"forward": lambda **k: ffn.forward(x, **k), "backward": lambda **k: ffn.backward(x, dy, **k),
+           "int8_ffn": lambda **k: i8.forward(x, **k), "linear": lambda **k: lin.forward(x, **k),
+           "quantize": lambda **k: pk.quantize_rows(x, **k)}[call]
+    as_tuple = lambda r: r if isinstance(r, tuple) else (r,)
+    want = [t.clone() for t in as_tuple(run())]
+    side = torch.cuda.Stream()
+    for nbytes in sorted({t.numel() * t.element_size() for t in want}):
+        behind_pending_work(nbytes)
+        got = as_tuple(run(stream=side.cuda_stream))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        del got
+    # the current stream, by its number
+    got = as_tuple(run(stream=torch.cuda.current_stream().cuda_stream))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for m in (ffn, i8, lin):
+        m.check()
+        m.close()
