@@ -222,6 +222,16 @@ def forward_static(x, logits, gate_up, down, num_experts: int, top_k: int, num_s
     return out
 
 
+def _empty(shape, dtype, device, stream: Optional[int]):
+    """A result for a call on `stream` (None: the current one), from that stream's memory: what lies in the current stream's may still
+    be written to by kernels that were launched there before."""
+    import torch
+    if stream is None or stream == torch.cuda.current_stream(device).cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 class WeaveMoE:
     """One MoE layer: weights [E+S,2I,H] / [E+S,H,I] bf16 on the GPU, a workspace, a handle."""
 
@@ -272,7 +282,7 @@ class WeaveMoE:
         assert logits.is_cuda and logits.dtype == torch.float32 and logits.is_contiguous()
         assert tuple(logits.shape) == (T, self.E)
         if out is None:
-            out = torch.empty_like(x)
+            out = _empty(x.shape, x.dtype, x.device, stream)
         if stream is None:
             stream = torch.cuda.current_stream(x.device).cuda_stream
         _check(self._lib.weave_moe_forward(self._h, x.data_ptr(), logits.data_ptr(), out.data_ptr(), T, stream),

@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 from typing import Optional
 
-from . import WeaveError, WEAVE_OK, _check, load as _load_library
+from . import WeaveError, WEAVE_OK, _check, _empty, load as _load_library
 
 BF16, F32, INT8 = 0, 1, 2
 
@@ -116,16 +116,6 @@ def _type_of(dtype):
         import torch
         _types.update({torch.bfloat16: BF16, torch.float32: F32, torch.int8: INT8})
     return _types[dtype]
-
-
-def _empty(shape, dtype, device, stream: Optional[int]):
-    """A result for a call on `stream` (None: the current one), from that stream's memory: what lies in the current stream's may still
-    be written to by kernels that were launched there before."""
-    import torch
-    if stream is None or stream == torch.cuda.current_stream(device).cuda_stream:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
-        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def quantize_rows(x, q=None, scale=None, stream: Optional[int] = None):

@@ -67,17 +67,24 @@ def test_the_largest_number_of_rows():
         assert torch.equal(s[at:at + part], (v.double().abs() / 127.0).float())
 
 
-def behind_pending_work(nbytes):
+@pytest.fixture(scope="module")
+def long_copy():
+    """A copy to the host of some 20 ms, which occupies no SM."""
+    src, dst = torch.zeros(1 << 30, dtype=torch.uint8, device="cuda"), torch.empty(1 << 30, dtype=torch.uint8, pin_memory=True)
+    return lambda: dst.copy_(src, non_blocking=True)
+
+
+def behind_pending_work(nbytes, long_copy):
     """Leaves the allocator a block of the current stream that a kernel, which has yet to run there, still writes to."""
     torch.cuda.synchronize()
     torch.cuda.empty_cache()
     block = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
-    torch.cuda._sleep(50_000_000)
+    long_copy()
     block.fill_(255)
 
 
 @pytest.mark.parametrize("call", ["forward", "backward", "int8_ffn", "linear", "quantize"])
-def test_results_of_a_call_on_a_given_stream(call):
+def test_results_of_a_call_on_a_given_stream(call, long_copy):
     """What a call allocates for its results is ordered by the stream that the call runs on, not by the current one."""
     T, H, I = 1000, 1040, 1056
     x, gate_up, down, dy = block(T, H, I, seed=63)
@@ -91,7 +98,7 @@ def test_results_of_a_call_on_a_given_stream(call):
     want = [t.clone() for t in as_tuple(run())]
     side = torch.cuda.Stream()
     for nbytes in sorted({t.numel() * t.element_size() for t in want}):
-        behind_pending_work(nbytes)
+        behind_pending_work(nbytes, long_copy)
         got = as_tuple(run(stream=side.cuda_stream))
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))

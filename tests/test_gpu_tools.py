@@ -143,3 +143,26 @@ def test_timeline_names_every_scheduled_tile_once(T):
         nt = cfg.I // geo["tile_n0"] + (cfg.H + geo["tile_n1"] - 1) // geo["tile_n1"]
         np.testing.assert_array_equal(np.sort(ev[(ev[:, 2] >> 24) == 5, 2] & 0xFFFFFF), np.arange(tiles * nt))
     moe.close()
+
+
+def test_results_of_a_call_on_a_given_stream():
+    """What a call allocates for its result is ordered by the stream that the call runs on, not by the current one, whose memory a
+    kernel that has yet to run may still write to."""
+    cfg = wl.MoEConfig("stream", 64, T=1000, H=1152, I=256, E=8, k=2)
+    x, lg, gu, dn = to_dev(wl.make_inputs(cfg))
+    moe = pk.WeaveMoE(gu, dn, cfg.E, cfg.k, cfg.S, max_tokens=cfg.T)
+    want = moe.forward(x, lg).clone()
+    moe.check()
+    side = torch.cuda.Stream()
+    src, dst = torch.zeros(1 << 30, dtype=torch.uint8, device="cuda"), torch.empty(1 << 30, dtype=torch.uint8, pin_memory=True)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    block = torch.empty(want.numel() * 2, dtype=torch.uint8, device="cuda")
+    dst.copy_(src, non_blocking=True)                    # some 20 ms, on no SM
+    block.fill_(255)
+    del block
+    got = moe.forward(x, lg, stream=side.cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    assert torch.equal(moe.forward(x, lg, stream=torch.cuda.current_stream().cuda_stream), want)
+    moe.close()
