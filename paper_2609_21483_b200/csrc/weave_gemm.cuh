@@ -158,10 +158,17 @@ __device__ __forceinline__ bool named_barrier_and(bool mine)
 
 // ------------------------------------------------------------------------------------ the activation
 
-// s = sigmoid(g).  exp overflows to inf for g below -88, where s is 0 either way; NaN and +inf come through.
-// __expf and the approximate division are off by 2^-21 and 2^-22 relative near 0 and by 2^-17 where |g| nears 88:
-// nothing next to the rounding to bf16 behind them.
-__device__ __forceinline__ float fast_sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
+// s = sigmoid(g) = (g < 0 ? e : 1) / (1 + e) with e = exp(-|g|): the divisor lies between 1 and 2, whatever g is, and s is a number
+// as small as fp32 has them (in 1 / (1 + exp(-g)) exp overflows from -88.7 on, and __fdividef() gives 0 for divisors above 2^126,
+// from -87.3 on: a large u makes these count).  NaN comes through.  __expf is off by 2^-21 relative near 0 and by 2^-17 where |g|
+// nears 88, the reciprocal by 2^-23: nothing next to the rounding to bf16 behind them.
+__device__ __forceinline__ float fast_sigmoid(float g)
+{
+    const float e = __expf(-fabsf(g));
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return (g < 0.0f ? e : 1.0f) * r;
+}
 __device__ __forceinline__ float gated(float g, float u) { return g * fast_sigmoid(g) * u; }
 
 // ------------------------------------------------------------------------------------ the kernel

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2609_21483_b200 as pk
-from test_gpu_ffn import block
+from test_gpu_ffn import ACT, BF16, block
 
 pytestmark = pytest.mark.gpu
 
@@ -110,3 +110,27 @@ def test_results_of_a_call_on_a_given_stream(call, long_copy):
     for m in (ffn, i8, lin):
         m.check()
         m.close()
+
+
+@pytest.mark.parametrize("T", [4, 200])
+def test_gates_that_are_almost_closed(T):
+    """sigmoid(g) where 1 + exp(-g) nears the largest fp32 number: tiny, but not zero, and a large u makes it count."""
+    H, I = 64, 64
+    gates = torch.tensor([-87.0, -87.5, -88.0, -88.5], device="cuda").repeat(T // 4)
+    x = torch.zeros(T, H, dtype=torch.bfloat16, device="cuda")
+    gate_up = torch.zeros(2 * I, H, dtype=torch.bfloat16, device="cuda")
+    down = torch.eye(H, I, dtype=torch.bfloat16, device="cuda")
+    gate_up[:I, 0], gate_up[I:, 1] = 1.0, 1.0
+    x[:, 0], x[:, 1] = gates, 2.0 ** 100
+    ffn = pk.GatedFFN(gate_up, down, max_tokens=T, backward=True)
+    y = ffn.forward(x)
+    dx, _, _ = ffn.backward(x, torch.ones_like(x))
+    ffn.check()
+    ffn.close()
+    g = gates.double()
+    s = torch.sigmoid(g)
+    # the activation is off by 2^-16, h (dg, du) and the result by a rounding to bf16 each; all terms of a sum are alike
+    off = lambda got, want: float((got.double() / want - 1).abs().max())
+    assert off(y, (g * s * 2.0 ** 100)[:, None]) <= 2 * BF16 + 2 * ACT
+    assert off(dx[:, 0], I * s * (1 + g * (1 - s)) * 2.0 ** 100) <= 2 * BF16 + 2 * ACT
+    assert off(dx[:, 1], I * g * s) <= 2 * BF16 + 2 * ACT
