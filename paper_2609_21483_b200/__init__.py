@@ -282,7 +282,7 @@ class WeaveMoE:
         assert logits.is_cuda and logits.dtype == torch.float32 and logits.is_contiguous()
         assert tuple(logits.shape) == (T, self.E)
         if out is None:
-            out = _empty(x.shape, x.dtype, x.device, stream)
+            out = torch.empty_like(x) if stream is None else _empty(x.shape, x.dtype, x.device, stream)
         if stream is None:
             stream = torch.cuda.current_stream(x.device).cuda_stream
         _check(self._lib.weave_moe_forward(self._h, x.data_ptr(), logits.data_ptr(), out.data_ptr(), T, stream),
