@@ -144,7 +144,7 @@ int engine_status(Engine &e, size_t control_bytes)
 
 // [rows][cols] row-major, rows `pitch` elements apart (0: cols), box of box_cols x box_rows
 bool map_2d(const Engine &e, CUtensorMap &m, int type, const void *p, long long rows, long long cols, int box_rows, int box_cols,
-            long long pitch = 0)
+            long long pitch = 0, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B)
 {
     const int size = type == WEAVE_BF16 ? 2 : type == WEAVE_F32 ? 4 : 1;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
@@ -154,8 +154,7 @@ bool map_2d(const Engine &e, CUtensorMap &m, int type, const void *p, long long 
     const CUtensorMapDataType dt = type == WEAVE_BF16  ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                    : type == WEAVE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                                        : CU_TENSOR_MAP_DATA_TYPE_UINT8;
-    return e.encode(&m, dt, 2, const_cast<void *>(p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    CU_TENSOR_MAP_SWIZZLE_128B,
+    return e.encode(&m, dt, 2, const_cast<void *>(p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // operand whose K runs along the rows' elements: some rows x 128 bytes
@@ -163,10 +162,12 @@ bool map_k(const Engine &e, CUtensorMap &m, int type, const void *p, long long r
 {
     return map_2d(e, m, type, p, rows, cols, box_rows, type == WEAVE_INT8 ? 128 : 64, pitch);
 }
-// operand whose K runs across the rows (bf16): 64 elements x 64 rows
-bool map_mn(const Engine &e, CUtensorMap &m, const void *p, long long rows, long long cols, long long pitch = 0)
+// operand whose K runs across the rows (bf16), of which a CTA takes `run` elements along them: boxes of one swizzle atom x 64 rows
+constexpr int mn_atom(int run) { return run % 64 == 0 ? 64 : 32; }
+bool map_mn(const Engine &e, CUtensorMap &m, const void *p, long long rows, long long cols, int run, long long pitch = 0)
 {
-    return map_2d(e, m, WEAVE_BF16, p, rows, cols, 64, 64, pitch);
+    return map_2d(e, m, WEAVE_BF16, p, rows, cols, 64, mn_atom(run), pitch,
+                  mn_atom(run) == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 // kBehind: launched while the launch before it in the stream, one of the same call, still runs (see pdl_wait())
@@ -504,7 +505,7 @@ struct Products {
     }
     void pairs(int M, int N, int width, int columns, int parts, bool b_mn)
     {
-        put({0, width * columns, 0, width, parts, 1, (int)gemm_tiles(M, N, width), b_mn ? width * columns / 2 : 0, b_mn ? 64 : 0});
+        put({0, width * columns, 0, width, parts, 1, (int)gemm_tiles(M, N, width), b_mn ? width * columns / 2 : 0, b_mn ? mn_atom(width * columns / 2) : 0});
     }
 };
 
@@ -688,7 +689,7 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     const uint8_t *up = static_cast<const uint8_t *>(h->cfg.gate_up) + (size_t)I * H * 2;
     const int rows_a = gemm_rows(T);
     const long long h_pitch = line_pitch(I), dgu_pitch = line_pitch(2ll * I);
-    bool ok = map_k(h->e, g.job[0].a, WEAVE_BF16, dy, T, H, rows_a) && map_mn(h->e, g.job[0].b[0], h->cfg.down, H, I) &&
+    bool ok = map_k(h->e, g.job[0].a, WEAVE_BF16, dy, T, H, rows_a) && map_mn(h->e, g.job[0].b[0], h->cfg.down, H, I, wide / 2) &&
               map_k(h->e, g.job[1].a, WEAVE_BF16, x, T, H, rows_a) && map_k(h->e, g.job[1].b[0], WEAVE_BF16, h->cfg.gate_up, I, H, wide) &&
               map_k(h->e, g.job[1].b[1], WEAVE_BF16, up, I, H, wide);
     if (!ok) return WEAVE_ERR_CUDA;
@@ -701,9 +702,9 @@ int weave_ffn_backward(weave_ffn_t h, const void *x, const void *dy, void *dx, v
     if (err != cudaSuccess) return cuda_fail(h->e, err);
     // dx = [dg du] W_gu, dW_gu = [dg du]^T x, dW_d = dy^T h: one launch, so that their last waves fill one another
     GemmArgs d;
-    ok = map_k(h->e, d.job[0].a, WEAVE_BF16, dgu, T, 2ll * I, rows_a, dgu_pitch) && map_mn(h->e, d.job[0].b[0], h->cfg.gate_up, 2ll * I, H) &&
-         map_mn(h->e, d.job[1].a, dgu, T, 2ll * I, dgu_pitch) && map_mn(h->e, d.job[1].b[0], x, T, H) &&
-         map_mn(h->e, d.job[2].a, dy, T, H) && map_mn(h->e, d.job[2].b[0], hbuf, T, I, h_pitch);
+    ok = map_k(h->e, d.job[0].a, WEAVE_BF16, dgu, T, 2ll * I, rows_a, dgu_pitch) && map_mn(h->e, d.job[0].b[0], h->cfg.gate_up, 2ll * I, H, plan.dx.width / 2) &&
+         map_mn(h->e, d.job[1].a, dgu, T, 2ll * I, 128, dgu_pitch) && map_mn(h->e, d.job[1].b[0], x, T, H, 128) &&
+         map_mn(h->e, d.job[2].a, dy, T, H, 128) && map_mn(h->e, d.job[2].b[0], hbuf, T, I, 128, h_pitch);
     if (!ok) return WEAVE_ERR_CUDA;
     for (int i = 0; i < 3; ++i) d.job[i].b[1] = d.job[i].b[0];
     gemm_job(d.job[0], T, H, 2ll * I, 64, plan.dx.width, false, true, dx, H, plan.dx.splits);

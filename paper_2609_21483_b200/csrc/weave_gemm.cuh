@@ -92,6 +92,12 @@ __device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t smem_addr)
 {
     return (uint64_t)((smem_addr >> 4) & 0x3FFFu) | (512ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
+// The same for boxes of 32 elements along MN, 64-byte swizzle: eight K rows are an atom of 512 bytes.  For operands of which a CTA has
+// only 32 along MN: half an atom of 64 is no layout that the instruction is defined for.
+__device__ __forceinline__ uint64_t umma_desc_mn_sw64(uint32_t smem_addr)
+{
+    return (uint64_t)((smem_addr >> 4) & 0x3FFFu) | (256ull << 16) | (32ull << 32) | (1ull << 46) | (4ull << 61);
+}
 // kind::i8: D int32 (2 at bit 4), A and B signed (1 at bits 7 and 10)
 __device__ __forceinline__ uint32_t umma_idesc_i8(uint32_t M, uint32_t N)
 {
@@ -185,8 +191,8 @@ struct alignas(64) GemmJob {
     int a_mn, b_mn;          // kEpiStore: operand is MN-major
     int rows;                // rows of A that a CTA takes of a tile, a multiple of 8 up to 128: a tile is 2 x rows high
     int width;               // columns of the result in a tile, up to 256 (gated 128): a product's N, twice that in the gated
-                             // forms, is a multiple of 16 in bf16 and of 32 in 8-bit integers.  Of 64 where B is MN-major
-                             // (kEpiGrad, too): with 16 of them in a CTA the products came out wrong, with 32 right
+                             // forms, is a multiple of 16 in bf16 and of 32 in 8-bit integers.  Where B is MN-major a CTA's half
+                             // of them is whole swizzle atoms: 64 or 128 in 128-byte swizzle, 32 (kEpiGrad) in 64-byte swizzle
     int tiles_m, tiles_n, group_m;
     int splits;              // parts of K that are worked on by different pairs (kEpiStore's job 0, not in kEpiGrad): fp32 or
                              // int32 sums in `partials`, added up in the order of K by whoever arrives last
@@ -460,12 +466,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                 const bool dh = kPhases == 2 && phase == 0;
                 const bool a_mn = kJobs && job.a_mn, b_mn = kJobs ? job.b_mn != 0 : dh;
                 const int half = kGatedTile && !dh ? job.width : job.width / 2;          // this CTA's rows of B
-                const int b_boxes = b_mn ? (half + 63) / 64 : 1;
-                const uint32_t tx = 2u * ((uint32_t)job.rows * 128u + (b_mn ? (uint32_t)b_boxes * 8192u : (uint32_t)half * 128u));
+                const uint32_t tx = 2u * (uint32_t)(job.rows + half) * 128u;
                 const void *map = load_a ? &job.a : &job.b[rank];
                 const int mn = load_a ? at.m0 + (int)rank * job.rows : at.n0 + (kGatedTile && !dh ? 0 : (int)rank * half);
                 const bool mn_major = load_a ? a_mn : b_mn;
-                const bool second = load_a ? a_mn : b_boxes == 2;
+                const bool second = load_a ? a_mn : b_mn && half == 128;
                 const int from = gemm_first<kSplit>(job, at), to = gemm_end<kSplit>(job, at);
                 for (int k = from; k < to; ++k) {
                     ok = __all_sync(0xffffffffu, ffn_wait(&bars.empty[s], ph ^ 1u, wc, 1 + warp));
@@ -506,7 +511,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                     const uint32_t n_mma = (uint32_t)(kGatedTile && !dh ? 2 * job.width : job.width);
                     const uint32_t idesc = (kI8 ? umma_idesc_i8(256, n_mma) : umma_idesc_bf16(256, n_mma)) | (a_mn ? kIdescAMn : 0u) |
                                            (b_mn ? kIdescBMn : 0u);
-                    const uint64_t a_inc = a_mn ? 128 : 2, b_inc = b_mn ? 128 : 2;
+                    const bool b_32 = dh && job.width == 64;
+                    const uint64_t a_inc = a_mn ? 128 : 2, b_inc = b_32 ? 64 : b_mn ? 128 : 2;
                     const int from = gemm_first<kSplit>(job, at), to = gemm_end<kSplit>(job, at);
                     for (int k = from; k < to; ++k) {
                         ok = __all_sync(0xffffffffu, ffn_wait(&bars.full[s], ph, wc, 4));
@@ -514,7 +520,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                         tc_fence_after();
                         const uint32_t a = smem + s * p.stage_bytes, b = a + p.a_bytes;      // (128 rows are read from a on, whatever lies there)
                         ffn_mma_kstep_pair<kI8>(d, a_mn ? umma_desc_mn_sw128(a) : umma_desc_sw128(a),
-                                                b_mn ? umma_desc_mn_sw128(b) : umma_desc_sw128(b), a_inc, b_inc, idesc, (uint32_t)(k != from),
+                                                b_32 ? umma_desc_mn_sw64(b) : b_mn ? umma_desc_mn_sw128(b) : umma_desc_sw128(b), a_inc, b_inc, idesc, (uint32_t)(k != from),
                                                 &bars.empty[s]);
                         if (++s == p.stages) { s = 0; ph ^= 1u; }
                     }

@@ -55,3 +55,15 @@ def test_plans_are_refused_for_what_calls_refuse():
         ffn.int8_linear_plan(24, 64, 8)
     with pytest.raises(ffn.WeaveError):
         ffn.int8_linear_plan(64, 64, 8, x_type=7)
+
+
+def test_operands_that_run_along_n_are_whole_swizzle_atoms():
+    """Where an operand's N (or M) runs along its rows, what a CTA gives to a product is whole atoms of its layout: 64 elements of
+    bf16 with 128-byte swizzle, 32 with 64-byte swizzle.  Columns that stick out over the matrix are zeros, not missing."""
+    seen = set()
+    for T, H, I in sizes(2, 8) + [(2, 64, 64), (257, 2048, 1408), (777, 1096, 2744), (4096, 4096, 14336)]:
+        for p in ffn.ffn_plan(H, I, T, backward=True):
+            if p["mn_run"]:
+                assert p["mn_atom"] in (32, 64) and p["mn_run"] % p["mn_atom"] == 0, (T, H, I, p)
+                seen.add((p["mn_run"], p["mn_atom"]))
+    assert seen == {(32, 32), (64, 64), (128, 64)}, seen
