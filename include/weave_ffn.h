@@ -85,8 +85,9 @@ typedef struct weave_ffn_product {
     int mn_run, mn_atom; /* where B's N runs along its rows: elements of it in a CTA, and in a swizzle atom; else 0 */
 } weave_ffn_product;
 int weave_ffn_debug_plan(const weave_ffn_config *cfg, int backward, int T, int n_sm, weave_ffn_product *out, int max_products);
-/* Test hook for the give-up path: thread block `cta` of a call of up to 128 tokens never arrives at a grid barrier, so the
- * bounded waits of all expire and the call ends with WEAVE_ERR_TIMEOUT (-1 = off, the default).  Nothing faults or traps. */
+/* Test hook for the give-up paths (-1 = off, the default).  In the one launch for up to 128 tokens thread block `cta` never
+ * arrives at a grid barrier, so that the bounded waits of all expire; in the launches on pairs of SMs the pair that it belongs to
+ * waits for bytes that nobody sends.  The call ends with WEAVE_ERR_TIMEOUT; nothing faults or traps. */
 int weave_ffn_debug_withhold_arrival(weave_ffn_t h, int cta);
 int weave_ffn_last_cuda_error(weave_ffn_t h);
 /* Releases host state.  Does not touch device memory. */

@@ -134,3 +134,30 @@ def test_gates_that_are_almost_closed(T):
     assert off(y, (g * s * 2.0 ** 100)[:, None]) <= 2 * BF16 + 2 * ACT
     assert off(dx[:, 0], I * s * (1 + g * (1 - s)) * 2.0 ** 100) <= 2 * BF16 + 2 * ACT
     assert off(dx[:, 1], I * g * s) <= 2 * BF16 + 2 * ACT
+
+
+@pytest.mark.parametrize("call,T,H,I", [("forward", 300, 520, 1032), ("forward", 257, 72, 6400), ("forward", 520, 8192, 208),
+                                        ("backward", 257, 2048, 1408), ("backward", 777, 520, 1032), ("backward", 596, 136, 4104),
+                                        ("int8_ffn", 300, 528, 1040), ("int8_ffn", 257, 80, 6400), ("int8_ffn", 520, 8192, 208)])
+def test_a_wait_on_pairs_that_gives_up_ends_the_call(call, T, H, I):
+    """One pair's stages never fill: its waits expire, those behind them see it, every launch of the call ends, and the handle works
+    again, with K in parts (where others had arrived) as without."""
+    x, gate_up, down, dy = block(T, H, I, seed=64)
+    if call == "int8_ffn":
+        ffn = pk.Int8FFN(*pk.quantize_rows(gate_up), *pk.quantize_rows(down), max_tokens=T)
+    else:
+        ffn = pk.GatedFFN(gate_up, down, max_tokens=T, backward=True)
+    run = (lambda: ffn.backward(x, dy)) if call == "backward" else (lambda: (ffn.forward(x),))
+    want = run()
+    ffn.check()
+    for cta in (0, 3):
+        ffn.set_timeout_ms(20)
+        ffn.debug_withhold_arrival(cta)
+        run()
+        assert ffn.status() == pk.ERR_TIMEOUT
+        ffn.debug_withhold_arrival(-1)
+        ffn.set_timeout_ms(4000)
+        for _ in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(run(), want))
+        ffn.check()
+    ffn.close()
