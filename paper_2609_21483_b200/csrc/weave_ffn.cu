@@ -427,7 +427,7 @@ cudaError_t launch_gemm(const Engine &e, GemmArgs &a, int jobs, int b_bytes, Lau
     a.ctl = e.ctl;
     a.timeout_ns = e.timeout_ns;
     a.partials = e.partials;
-    a.withhold = e.withhold < 0 ? -1 : e.withhold / 2;
+    a.withhold = e.withhold < 0 ? ~0u : (unsigned)e.withhold & ~1u;
     a.a_bytes = 0;
     for (int i = 0; i < jobs; ++i) a.a_bytes = a.job[i].rows * 128 > a.a_bytes ? a.job[i].rows * 128 : a.a_bytes;
     a.stage_bytes = a.a_bytes + b_bytes;

@@ -208,7 +208,7 @@ struct alignas(64) GemmArgs {
     int out_f32, direct;     // kEpiScaled: type of the result; 1 = row length not a multiple of 16 bytes
     int extra;               // kEpiStore: see gemm_tile()
     int stages, a_bytes, stage_bytes;
-    int withhold;            // test hook: this pair's stages wait for bytes that nobody sends (-1: none)
+    unsigned withhold;       // test hook: the first CTA of a pair whose stages wait for bytes that nobody sends (none: all ones)
 };
 
 constexpr int kGemmThreads = 384;                   // two producers, the issuer, one idle warp, eight epilogue warps
@@ -457,7 +457,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
         // ---- producers: warp 0 brings this CTA's rows of A, warp 1 its part of B; all bytes of a stage are credited
         // to the full barrier in the pair's leader
         const bool load_a = warp == 0;
-        const uint32_t missing = pair == p.withhold ? 16u : 0u;
         pdl_wait();
         fence_proxy_async_global();      // what the launch before wrote with ordinary stores is read by tensor copies
         int s = 0;
@@ -468,7 +467,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) wea
                 const bool dh = kPhases == 2 && phase == 0;
                 const bool a_mn = kJobs && job.a_mn, b_mn = kJobs ? job.b_mn != 0 : dh;
                 const int half = kGatedTile && !dh ? job.width : job.width / 2;          // this CTA's rows of B
-                const uint32_t tx = 2u * (uint32_t)(job.rows + half) * 128u + missing;
+                const uint32_t tx = 2u * (uint32_t)(job.rows + half) * 128u + ((blockIdx.x & ~1u) == p.withhold ? 16u : 0u);
                 const void *map = load_a ? &job.a : &job.b[rank];
                 const int mn = load_a ? at.m0 + (int)rank * job.rows : at.n0 + (kGatedTile && !dh ? 0 : (int)rank * half);
                 const bool mn_major = load_a ? a_mn : b_mn;
