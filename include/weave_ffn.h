@@ -48,7 +48,8 @@ typedef struct weave_ffn_config {
  * (max_tokens above 32 or the gradient, and H up to 4736 or I up to 2368). */
 size_t weave_ffn_workspace_bytes(const weave_ffn_config *cfg);
 
-/* Validates the config, encodes the weights' TMA descriptors, zeroes the control words (synchronous). */
+/* Validates the config and zeroes the control words, behind all work given to the device before (synchronous, so not to be called
+ * while a stream is being captured).  Tensor maps are encoded by each call, on the host: their boxes depend on T. */
 int weave_ffn_create(const weave_ffn_config *cfg, weave_ffn_t *out_handle);
 
 /* out[t] = Wd ( silu(Wg x[t]) (.) Wu x[t] ), x and out bf16 [T][H], 0 <= T <= max_tokens.

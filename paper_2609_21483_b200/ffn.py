@@ -203,7 +203,10 @@ def _need_cuda(what: str):
 
 class GatedFFN(_Handle):
     """The dense block down(silu(gate x) * (up x)) in bf16: gate_up [2I, H] (gate rows, then up rows), down [H, I], on
-    the GPU.  backward=True reserves what backward() needs (6 T I bytes instead of 2 T I)."""
+    the GPU.  backward=True reserves what backward() needs (6 T I bytes instead of 2 T I).
+
+    No operator of autograd: forward()'s result carries no graph, whatever x or the weights require, and backward() is called
+    by the training step itself; it overwrites its results, so that gradients of several micro-batches are added up outside."""
 
     _name = "weave_ffn"
 
