@@ -226,6 +226,8 @@ def _empty(shape, dtype, device, stream: Optional[int]):
     """A result for a call on `stream` (None: the current one), from that stream's memory: what lies in the current stream's may still
     be written to by kernels that were launched there before."""
     import torch
+    if stream == 1:              # cudaStreamLegacy: another name of 0, which PyTorch does not know
+        stream = 0
     if stream is None or stream == torch.cuda.current_stream(device).cuda_stream:
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):

@@ -175,6 +175,8 @@ __device__ __forceinline__ float fast_sigmoid(float g)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
     return (g < 0.0f ? e : 1.0f) * r;
 }
+// Where h, dg or du are an operand of the next product they are rounded to bf16, the type of the other operand: 0.0024 of a result's
+// size in the root of the mean square instead of the 0.0017 that its own rounding makes.
 __device__ __forceinline__ float gated(float g, float u) { return g * fast_sigmoid(g) * u; }
 
 // ------------------------------------------------------------------------------------ the kernel

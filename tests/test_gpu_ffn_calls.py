@@ -161,3 +161,18 @@ def test_a_wait_on_pairs_that_gives_up_ends_the_call(call, T, H, I):
             assert all(torch.equal(a, b) for a, b in zip(run(), want))
         ffn.check()
     ffn.close()
+
+
+def test_streams_by_their_special_names():
+    """The default stream as 0 and as cudaStreamLegacy (1), the thread's own (2), while another stream is current."""
+    x, gate_up, down, dy = block(200, 264, 136, seed=65)
+    ffn = pk.GatedFFN(gate_up, down, max_tokens=200, backward=True)
+    want = (ffn.forward(x), *ffn.backward(x, dy), *pk.quantize_rows(x))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        for stream in (0, 1, 2):
+            got = (ffn.forward(x, stream=stream), *ffn.backward(x, dy, stream=stream), *pk.quantize_rows(x, stream=stream))
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+    ffn.check()
+    ffn.close()
