@@ -176,3 +176,21 @@ def test_streams_by_their_special_names():
             assert all(torch.equal(a, b) for a, b in zip(got, want))
     ffn.check()
     ffn.close()
+
+
+@pytest.mark.parametrize("T", [2, 5, 200])
+def test_a_row_with_nan_marks_itself_alone(T):
+    """In both blocks: the others are the bits that they are without it, and a row of zeros gives zeros."""
+    H, I = 272, 400
+    x, gate_up, down, _ = block(T, H, I, seed=66)
+    gq, gs, dq, ds = *pk.quantize_rows(gate_up), *pk.quantize_rows(down)
+    for ffn in (pk.GatedFFN(gate_up, down, max_tokens=T), pk.Int8FFN(gq, gs, dq, ds, max_tokens=T)):
+        want = ffn.forward(x)
+        for bad in (float("nan"), float("inf"), -float("inf")):
+            y = x.clone()
+            y[T - 1, 7] = bad
+            y[0] = 0
+            got = ffn.forward(y)
+            ffn.check()
+            assert bool(torch.isnan(got[T - 1]).all()) and not bool(got[0].any()) and torch.equal(got[1:T - 1], want[1:T - 1])
+        ffn.close()
